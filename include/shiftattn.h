@@ -224,6 +224,153 @@ int sp_decode_step(const sp_cache_desc *cache, const void *k_new, const void *v_
                    int32_t max_seq_len, int32_t num_q_heads, float scale, void *workspace,
                    size_t workspace_bytes, void *stream);
 
+/*
+ * sp_attn_cross — attention of every sequence's query tokens to ALL of its cached states: a decoder's cross attention to
+ * an encoder's states (of another length than the queries), or an encoder's own layers.  No causal mask; the states
+ * were appended by sp_kv_append (or sp_norm_rope_append) and stay where they are from step to step.
+ *   q, out          bf16 [total_q_tokens][num_q_heads][head_dim], packed by sequence
+ *   cu_seqlens_q    int32 [batch + 1]
+ *   kv_lens         int32 [batch] cached states of each sequence; every query of sequence s sees the states
+ *                   0 .. kv_lens[s] - 1.  A sequence with kv_lens[s] <= 0 gets all-zero output rows
+ *   max_q_len, max_kv_len  host hints: >= the longest chunk and >= the largest kv_lens[s] (not detected if too small:
+ *                   rows beyond max_q_len are not computed, states beyond max_kv_len may be ignored)
+ *   workspace       optional device scratch; with sp_attn_cross_workspace_size(...) bytes, long key ranges of few query
+ *                   tokens are divided over workgroups and merged, as in sp_attn_prefill.  Without it, or with less, they are not
+ *                   or into fewer pieces: the same result up to fp32 summation order
+ * Sequences without query tokens, and sub-ranges of a batch, as in sp_attn_prefill.  Hypotheses of a beam search that share
+ * an encoder are best passed as the query tokens of one sequence: its states are then read once for all of them.  Batches
+ * of exactly one token per sequence may as well call sp_attn_decode with kv_lens as seq_lens.  Arithmetic and error bound:
+ * as for sp_attn_prefill.
+ */
+int sp_attn_cross(const sp_cache_desc *cache, const void *q, void *out, const int32_t *cu_seqlens_q,
+                  const int32_t *kv_lens, const int32_t *block_table, int32_t batch,
+                  int32_t max_pages_per_seq, int32_t total_q_tokens, int32_t max_q_len,
+                  int32_t max_kv_len, int32_t num_q_heads, float scale, void *workspace,
+                  size_t workspace_bytes, void *stream);
+size_t sp_attn_cross_workspace_size(int32_t batch, int32_t total_q_tokens, int32_t max_q_len,
+                                    int32_t max_kv_len, int32_t num_q_heads, int32_t num_kv_heads,
+                                    int32_t head_dim);
+
+/* Rotation of position-dependent channel pairs (sp_norm_rope_append).  The struct is read on the HOST at call time. */
+typedef struct sp_rope_desc {
+  const float *cos_sin;   /* device, fp32 [num_positions][rotary_dim]: rotary_dim / 2 cosines of a position's angles,
+                             then as many sines                                                                   */
+  int32_t num_positions;
+  int32_t rotary_dim;     /* the first channels of a row are rotated: a multiple of 16 up to head_dim             */
+  int32_t interleaved;    /* pair i of the angles is channels (i, i + rotary_dim / 2) if 0, (2i, 2i + 1) if 1     */
+} sp_rope_desc;
+
+/*
+ * sp_norm_rope_append — the step between the projections and the attention, in one pass: every head's queries and keys are
+ * normalised by their root mean square and rotated by their position's angles, the queries are packed for the attention
+ * call, the keys and the (unchanged) values are written to their pages as sp_kv_append would.
+ *   q, k, v         bf16; token t's rows begin at element t * q_stride (k_stride, v_stride), its heads follow each other
+ *                   ([heads][head_dim]): separate tensors, or parts of one fused projection's rows
+ *   q_out           bf16 [total_new_tokens][num_q_heads][head_dim].  May be q itself if its tokens are packed; any other
+ *                   overlap with q, k or v is refused
+ *   q_weight, k_weight  bf16 [head_dim], each NULL for no normalisation of queries or keys:
+ *                   y = x / sqrt(mean(x^2) + eps) * weight
+ *   rope            NULL for no rotation.  Pair (a, b) of channels becomes (a cos - b sin, b cos + a sin)
+ *   positions       int32 [total_new_tokens] rows of cos_sin, or NULL: a token's position in its sequence.  Rows outside
+ *                   the table are bad metadata (the nearest row is taken)
+ *   cu_seqlens_new, ctx_lens, block_table, batch, max_pages_per_seq, total_new_tokens, sub-ranges: as in sp_kv_append
+ *   num_q_heads     any number; 0 (q and q_out NULL): keys and values only, an encoder's states for example
+ *   k, v            both NULL: queries only (block_table may be NULL then)
+ * Sums and products in fp32, one rounding to bf16 at the end; rows that are neither normalised nor rotated keep their values.
+ */
+int sp_norm_rope_append(const sp_cache_desc *cache, const void *q, const void *k, const void *v,
+                        int64_t q_stride, int64_t k_stride, int64_t v_stride, void *q_out,
+                        const void *q_weight, const void *k_weight, float eps,
+                        const sp_rope_desc *rope, const int32_t *positions,
+                        const int32_t *cu_seqlens_new, const int32_t *ctx_lens,
+                        const int32_t *block_table, int32_t batch, int32_t max_pages_per_seq,
+                        int32_t total_new_tokens, int32_t num_q_heads, void *stream);
+
+/*
+ * Pages of a cache, on the device: which pages a sequence holds, how many sequences hold a page.  One table serves the caches
+ * of all layers.  The calls below keep it without the host: they can be captured with the step.  The struct is read on the
+ * HOST at call time; its arrays belong to the caller.
+ * What every call keeps true, given that it was true before: a row s holds the pages of its first
+ * ceil(seq_lens[s] / 16) entries; ref_counts[p] is the number of entries that hold page p; a page is free if that is 0.
+ * Free pages are always taken in ascending order, for the entries of a call's list in their order: results do not
+ * depend on timing.
+ * Out-of-range rows and page ids are skipped; lengths count as at most max_pages_per_seq * 16.
+ */
+typedef struct sp_page_table {
+  int32_t *ref_counts;  /* device, int32 [num_pages]                                            */
+  int32_t *block_table; /* device, int32 [num_rows][max_pages_per_seq], what the attention reads */
+  int32_t *seq_lens;    /* device, int32 [num_rows] tokens that the row has room for            */
+  int32_t num_pages;
+  int32_t num_rows;
+  int32_t max_pages_per_seq;
+} sp_page_table;
+
+/*
+ * sp_pages_reserve — room for more tokens: row rows[i] grows to new_lens[i] tokens (if it has fewer) and gets the pages
+ * that this takes.  All entries or none: if the pool has too few free pages nothing changes.  Entries longer than a table row
+ * are skipped.  The rows are distinct (of several entries for one row, unspecified ones get their room).
+ *   shortfall  int32 [1] (device, written): pages that were missing, 0 if the call has been carried out
+ *   workspace  sp_pages_workspace_size(num_pages, n) bytes, contents need no initialisation
+ */
+int sp_pages_reserve(const sp_page_table *table, const int32_t *rows, const int32_t *new_lens, int32_t n,
+                     int32_t *shortfall, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * sp_pages_fork — row children[i] becomes a copy of row parents[i]: it holds the same full pages, and if the parent's last page
+ * is not full, a page of its own for it, whose rows the caller copies with sp_pages_copy in the cache of every layer:
+ *   copy_src, copy_dst, copy_rows  int32 [n] (device, written): rows 0 .. copy_rows[i] - 1 of page copy_src[i] belong into
+ *              page copy_dst[i]; -1, -1 and 0 where there is nothing to copy
+ * A child is an empty row (seq_lens 0), and named once; entries whose child is not empty are skipped, and of several entries
+ * for one child an unspecified one is taken.  All entries or none, shortfall and workspace: as in sp_pages_reserve.
+ */
+int sp_pages_fork(const sp_page_table *table, const int32_t *parents, const int32_t *children, int32_t n,
+                  int32_t *copy_src, int32_t *copy_dst, int32_t *copy_rows, int32_t *shortfall,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * sp_pages_release — row rows[i] keeps its first keep_lens[i] tokens (keep_lens NULL: none): the pages behind them are
+ * given back (their entries become -1), and free again if no other row holds them.  A row may be named several times: it
+ * keeps the least.
+ */
+int sp_pages_release(const sp_page_table *table, const int32_t *rows, const int32_t *keep_lens, int32_t n,
+                     void *stream);
+
+/*
+ * sp_pages_compact — moves the pages in use to the front of the pool: with U of them, the i-th page in use from U on goes
+ * to the i-th free page below U.
+ *   new_block_table, new_ref_counts  as the table's arrays; may be the table's own.  Only entries that hold a page are
+ *              written.  With others, the old ones stay valid until the caller drops them: the moved pages' bytes are not
+ *              overwritten by the moves
+ *   move_src, move_dst  int32 [num_pages / 2] (device, written up to the number of moves): what the caller copies with
+ *              sp_pages_copy, in the cache of every layer, before the new table is used
+ *   moved      int32 [2] (device, written): number of moves; U
+ *   workspace  sp_pages_workspace_size(num_pages, 0) bytes
+ */
+int sp_pages_compact(const sp_page_table *table, int32_t *new_block_table, int32_t *new_ref_counts,
+                     int32_t *move_src, int32_t *move_dst, int32_t *moved, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
+/*
+ * sp_pages_copy — copies pages inside caches: in each of num_caches caches (one per layer, all with the same numbers of
+ * pages and heads and the same head_dim), rows 0 .. rows[i] - 1 of page src[i], K and V, all heads, to page dst[i].
+ *   src, dst   int32 [n] (device); pairs with an id outside the pool are skipped
+ *   rows       int32 [n] (device), or NULL: whole pages
+ *   count      int32 [1] (device), or NULL: only the first min(n, count) pairs
+ * No page is the source of one pair and the destination of another, or the destination of two: the pairs are copied in no
+ * particular order.
+ */
+int sp_pages_copy(const sp_cache_desc *caches, int32_t num_caches, const int32_t *src, const int32_t *dst,
+                  const int32_t *rows, const int32_t *count, int32_t n, void *stream);
+
+/* Bytes of workspace of sp_pages_reserve and sp_pages_fork with up to n entries (n > 0), or of sp_pages_compact (n = 0). */
+size_t sp_pages_workspace_size(int32_t num_pages, int32_t n);
+
+/*
+ * sp_debug_validate_pages — SYNCHRONOUS test helper: copies the table to the host and checks what the page calls keep true
+ * (see sp_page_table).  Returns SP_OK or SP_ERR_BAD_SHAPE with the first violation in sp_last_error().
+ */
+int sp_debug_validate_pages(const sp_page_table *table);
+
 /* Bytes of workspace for the given host-side shape: what sp_attn_decode requires, and what lets
  * sp_attn_prefill split key ranges or take its short-chunk path (0 when neither would be used:
  * too many query rows for it to pay).  max_q_len / max_kv_len are the hints later passed to

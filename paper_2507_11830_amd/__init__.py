@@ -33,6 +33,8 @@ SP_ERR_HIP = -5
 
 EXPORTS = (
     "sp_kv_append", "sp_attn_prefill", "sp_attn_decode", "sp_attn_decode_static", "sp_decode_step", "sp_chunk_step", "sp_ulysses_pack", "sp_ulysses_unpack",
+    "sp_attn_cross", "sp_norm_rope_append", "sp_pages_reserve", "sp_pages_fork", "sp_pages_release", "sp_pages_compact", "sp_pages_copy",
+    "sp_attn_cross_workspace_size", "sp_pages_workspace_size", "sp_debug_validate_pages",
     "sp_attn_prefill_workspace_size",
     "sp_attn_decode_workspace_size", "sp_debug_validate_metadata", "sp_debug_validate_hints", "sp_debug_set_tuning",
     "sp_status_string", "sp_last_error", "sp_version",
@@ -52,6 +54,17 @@ class sp_cache_desc(ctypes.Structure):
     ]
 
 
+class sp_rope_desc(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("num_positions", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class sp_page_table(ctypes.Structure):
+    _fields_ = [
+        ("ref_counts", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("num_pages", ctypes.c_int32),
+        ("num_rows", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+    ]
+
+
 _lib = None
 _native = None
 
@@ -67,8 +80,10 @@ def _bind(L: ctypes.CDLL):
     module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_binding", loader))
     loader.exec_module(module)
     names = ("sp_kv_append", "sp_attn_prefill", "sp_chunk_step", "sp_attn_decode", "sp_attn_decode_static", "sp_decode_step")
+    names += tuple(n for n in ("sp_attn_cross", "sp_norm_rope_append", "sp_pages_reserve", "sp_pages_fork", "sp_pages_release", "sp_pages_compact",
+                               "sp_pages_copy") if hasattr(L, n))
     module.bind({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names}, ctypes.ArgumentError, ctypes.c_int32, sp_cache_desc,
-                torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.cuda.current_stream)
+                torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.cuda.current_stream, sp_page_table)
     _native = module
     return module
 
@@ -109,6 +124,28 @@ def lib() -> ctypes.CDLL:
         L.sp_chunk_step.argtypes = [cd, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
                                     ctypes.c_float, vp, sz, vp]
         L.sp_chunk_step.restype = ctypes.c_int
+        L.sp_attn_cross.argtypes = [cd, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, ctypes.c_float, vp, sz, vp]
+        L.sp_attn_cross.restype = ctypes.c_int
+        L.sp_attn_cross_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32]
+        L.sp_attn_cross_workspace_size.restype = sz
+        i64, pt = ctypes.c_int64, ctypes.POINTER(sp_page_table)
+        L.sp_norm_rope_append.argtypes = [cd, vp, vp, vp, i64, i64, i64, vp, vp, vp, ctypes.c_float, ctypes.POINTER(sp_rope_desc), vp, vp, vp, vp,
+                                          i32, i32, i32, i32, vp]
+        L.sp_norm_rope_append.restype = ctypes.c_int
+        L.sp_pages_reserve.argtypes = [pt, vp, vp, i32, vp, vp, sz, vp]
+        L.sp_pages_reserve.restype = ctypes.c_int
+        L.sp_pages_fork.argtypes = [pt, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.sp_pages_fork.restype = ctypes.c_int
+        L.sp_pages_release.argtypes = [pt, vp, vp, i32, vp]
+        L.sp_pages_release.restype = ctypes.c_int
+        L.sp_pages_compact.argtypes = [pt, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.sp_pages_compact.restype = ctypes.c_int
+        L.sp_pages_copy.argtypes = [cd, i32, vp, vp, vp, vp, i32, vp]
+        L.sp_pages_copy.restype = ctypes.c_int
+        L.sp_pages_workspace_size.argtypes = [i32, i32]
+        L.sp_pages_workspace_size.restype = sz
+        L.sp_debug_validate_pages.argtypes = [pt]
+        L.sp_debug_validate_pages.restype = ctypes.c_int
         L.sp_ulysses_pack.argtypes = [vp, vp, i32, i32, i32, i32, vp]
         L.sp_ulysses_pack.restype = ctypes.c_int
         L.sp_ulysses_unpack.argtypes = [vp, vp, i32, i32, i32, i32, vp]
@@ -185,6 +222,29 @@ class KVCache:
         return self.desc.head_dim
 
 
+class PageTable:
+    """Which pages every row (sequence) of a block table holds, and how many entries hold a page: int32 cuda tensors
+    block_table [rows, max_pages], seq_lens [rows], ref_counts [num_pages], plus the C descriptor that names them."""
+
+    def __init__(self, block_table, seq_lens, ref_counts):
+        import torch
+
+        for t in (block_table, seq_lens, ref_counts):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.int32
+        rows, max_pages = block_table.shape
+        assert seq_lens.shape == (rows,) and ref_counts.dim() == 1
+        self.block_table, self.seq_lens, self.ref_counts = block_table, seq_lens, ref_counts
+        self.desc = sp_page_table(ref_counts.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), ref_counts.shape[0], rows, max_pages)
+
+    @classmethod
+    def empty(cls, num_rows: int, max_pages: int, num_pages: int, device="cuda:0"):
+        """No row holds a page."""
+        import torch
+
+        return cls(torch.full((num_rows, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(num_rows, dtype=torch.int32, device=device), torch.zeros(num_pages, dtype=torch.int32, device=device))
+
+
 def sp_version() -> int:
     return lib().sp_version()
 
@@ -237,6 +297,61 @@ def sp_chunk_step(cache: KVCache, k_new, v_new, q, out, cu_seqlens_q, ctx_lens, 
     sp_attn_prefill."""
     _check((_native or _calls()).chunk_step(cache, k_new, v_new, q, out, cu_seqlens_q, ctx_lens, block_table, max_q_len, max_kv_len,
                                             scale, workspace, stream))
+
+
+def sp_attn_cross_workspace_size(batch: int, total_q_tokens: int, max_q_len: int, max_kv_len: int, num_q_heads: int,
+                                 num_kv_heads: int, head_dim: int) -> int:
+    return lib().sp_attn_cross_workspace_size(batch, total_q_tokens, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim)
+
+
+def sp_attn_cross(cache: KVCache, q, out, cu_seqlens_q, kv_lens, block_table, max_q_len: int, max_kv_len: int, scale: float,
+                  workspace=None, stream=None) -> None:
+    """q, out: bf16 [T, Hq, d] (cuda).  Every query of sequence s sees all kv_lens[s] cached states."""
+    _check((_native or _calls()).attn_cross(cache, q, out, cu_seqlens_q, kv_lens, block_table, max_q_len, max_kv_len, scale, workspace, stream))
+
+
+def sp_norm_rope_append(cache: KVCache, q, k, v, q_out, cu_seqlens_new, ctx_lens, block_table, q_weight=None, k_weight=None,
+                        eps: float = 1e-6, cos_sin=None, interleaved: bool = False, positions=None, stream=None) -> None:
+    """q [T, Hq, d], k, v [T, Hkv, d]: bf16 (cuda), also parts of one fused projection [T, Hq + 2 Hkv, d]; q_out bf16 [T, Hq, d].
+    q_weight, k_weight: bf16 [d] of the norms, or None; cos_sin: fp32 [positions, rotary_dim], or None; positions: int32 [T], or
+    None.  q and q_out None: keys and values only; k and v None: queries only (block_table may be None too)."""
+    _check((_native or _calls()).norm_rope_append(cache, q, k, v, q_out, cu_seqlens_new, ctx_lens, block_table, q_weight, k_weight, eps, cos_sin,
+                                                  interleaved, positions, stream))
+
+
+def sp_pages_workspace_size(num_pages: int, n: int) -> int:
+    return lib().sp_pages_workspace_size(num_pages, n)
+
+
+def sp_pages_reserve(table: PageTable, rows, new_lens, shortfall, workspace, stream=None) -> None:
+    """rows, new_lens: int32 [n]; shortfall: int32 [1], pages that were missing (then nothing has changed)."""
+    _check((_native or _calls()).pages_reserve(table, rows, new_lens, shortfall, workspace, stream))
+
+
+def sp_pages_fork(table: PageTable, parents, children, copy_src, copy_dst, copy_rows, shortfall, workspace, stream=None) -> None:
+    """All int32 [n], shortfall [1].  The copies that are asked for in copy_* are made by sp_pages_copy."""
+    _check((_native or _calls()).pages_fork(table, parents, children, copy_src, copy_dst, copy_rows, shortfall, workspace, stream))
+
+
+def sp_pages_release(table: PageTable, rows, keep_lens=None, stream=None) -> None:
+    """rows, keep_lens: int32 [n]; without keep_lens the rows are emptied."""
+    _check((_native or _calls()).pages_release(table, rows, keep_lens, stream))
+
+
+def sp_pages_compact(table: PageTable, new_block_table, new_ref_counts, move_src, move_dst, moved, workspace, stream=None) -> None:
+    """new_*: as the table's arrays, or these themselves; move_src, move_dst: int32 [num_pages // 2]; moved: int32 [2], the number of
+    moves (what sp_pages_copy takes as count) and of pages in use."""
+    _check((_native or _calls()).pages_compact(table, new_block_table, new_ref_counts, move_src, move_dst, moved, workspace, stream))
+
+
+def sp_pages_copy(caches, src, dst, rows=None, count=None, stream=None) -> None:
+    """caches: a KVCache or a sequence of them, all of one shape (the layers'); src, dst, rows: int32 [n]; count: int32 [1] or None."""
+    _check((_native or _calls()).pages_copy((caches,) if isinstance(caches, KVCache) else caches, src, dst, rows, count, stream))
+
+
+def sp_debug_validate_pages(table: PageTable) -> None:
+    """Synchronous check that every page's count is the number of entries that hold it."""
+    _check(lib().sp_debug_validate_pages(ctypes.byref(table.desc)))
 
 
 def sp_debug_validate_metadata(cache: KVCache, seq_lens, block_table) -> None:

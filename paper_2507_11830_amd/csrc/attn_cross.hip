@@ -1,0 +1,138 @@
+// Attention without a mask over the paged cache (sp_attn_cross): every query token of a sequence sees all of its states, those of an
+// encoder of another length.
+//
+//   out[t] = sum_j p_tj v_j,  p_t = softmax_j(scale q_t . k_j),  j = 0 .. kv_lens[s] - 1; zeros where there are none
+//
+// The kernels are those of the causal calls with another limit on a column's keys (CrossArgs in prefill_tile.h, CROSS in
+// decode_stream.h): no tile is masked but a sequence's last, all query tiles of a sequence are equally long, and rows without
+// keys are written as zeros.  Bound: bf16 MFMA, 4 * head_dim operations per (query, key) pair and head, for long chunks; HBM, the
+// states once for all query heads and tokens, for chunks of a few tokens.
+//
+// What is chosen from the hints, by the same measured rules as in attn_prefill.hip where the question is the same:
+//   - chunks of a few tokens (one or two column tiles of a wave): the decode kernel with equal shares or fixed splits;
+//   - otherwise query tiles of 256 columns (128 at head_dim 64, several workgroups a CU); on grids that do not fill the chip, of 128
+//     columns whose two wave groups take alternate key tiles, and where even these leave most CUs idle and the key ranges
+//     are long, in pieces of the key range.
+#include "decode_stream.h"
+#include "prefill_solo.h"
+
+namespace sp {
+
+// ---- chunks of a few tokens
+template <int D, int NT>
+__global__ __launch_bounds__(64 * kWaves, NT > 1 ? 1 : 2) void cross_stream_kernel(DecodeArgs a) {
+  extern __shared__ __align__(16) char smem_raw[];
+  lds_char *smem = (lds_char *)smem_raw;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (a.row_splits) {  // fixed splits of a.chunk keys
+    const int hg = blockIdx.x, seq = blockIdx.y, split = blockIdx.z;
+    const int p0 = split * (a.chunk >> 5);
+    const int pages = load_pages(a, seq, p0, 0, w, lane);  // in the same round trip as the lengths
+    const int tok = a.cu_q[seq], qn = a.cu_q[seq + 1] - tok, L = cross_keys(a, a.ctx_lens[seq]);
+    if (qn <= 0) return;
+    const int p1 = min((L + 31) >> 5, p0 + (a.chunk >> 5)), slot = (seq * a.n_hgroups + hg) * a.row_splits + split;
+    if (p1 <= p0) {  // no keys: rows of zeros if there is no other split, else an empty partial
+      if (a.row_splits == 1) zero_chunk<D>(a, tok, qn, hg);
+      else if ((int)threadIdx.x < a.cols) *reinterpret_cast<f32x2 *>(a.part_ml + 2 * ((long)slot * a.cols + threadIdx.x)) = (f32x2){-INFINITY, 0.f};
+      return;
+    }
+    row_segment<D, false, true, NT, true>(a, smem, lane, w, seq, hg, L, L - qn, tok, p0, p1, pages, a.row_splits == 1, slot);
+    return;
+  }
+  decode_share<D, false, true, NT, true>(a, smem, lane, w, blockIdx.x);
+}
+
+template <int D, int NT>
+static int launch_cross_stream(const DecodeArgs &a, dim3 wgs, int max_pieces, hipStream_t stream) {
+  static bool done = false;
+  constexpr int smem = kDecodeShareSmem<D, true>;
+  if (int rc = grant_smem((const void *)cross_stream_kernel<D, NT>, &done, smem)) return rc;
+  hipLaunchKernelGGL((cross_stream_kernel<D, NT>), wgs, dim3(64 * kWaves), smem, stream, a);
+  if (a.row_splits != 1) launch_decode_combine(a, max_pieces, D, stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SP_OK : fail(SP_ERR_HIP, "sp_attn_cross launch: %s", hipGetErrorString(e));
+}
+
+// ---- longer chunks
+template <int D>
+static int launch_cross_d(const CrossArgs &a, bool split, int batch, int max_q_len, hipStream_t stream) {
+  constexpr size_t smem = kPrefillSmem<D>;
+  static bool set[3] = {false, false, false};
+  if (a.kv_splits > 1) return launch_cfg(prefill_kernel<D, KVT, PFD, true, true, 0, CrossArgs>, &set[0], 2 * smem, 128, a, batch, max_q_len, stream);
+  if (split) return launch_cfg(prefill_kernel<D, KVT, PFD, true, false, 0, CrossArgs>, &set[1], 2 * smem, 128, a, batch, max_q_len, stream);
+  if constexpr (D == 64) return launch_cfg(solo_prefill_kernel<CrossArgs>, &set[2], kSoloSmem, kSoloCols, a, batch, max_q_len, stream, kSoloThreads, kSoloLayers);
+  else return launch_cfg(prefill_kernel<D, KVT, PFD, false, false, 0, CrossArgs>, &set[2], smem, 256, a, batch, max_q_len, stream);
+}
+
+static int column_shift(int group) {  // log2 of the heads that share the column dimension
+  int gshift = 0;
+  if ((group & (group - 1)) == 0)
+    while ((1 << gshift) < group && gshift < 5) ++gshift;
+  return gshift;
+}
+
+// Pieces of the key ranges of a launch of long chunks.
+static int cross_pieces(long rows, long wg128, int max_kv_len) {
+  if (!is_small_grid(wg128)) return 1;
+  const int kvs = kv_pieces(wg128, max_kv_len), cap = kv_split_cap(rows);
+  return kvs < 1 ? 1 : kvs < cap ? kvs : cap;
+}
+
+size_t cross_workspace_bytes(int batch, int total_q, int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim) {
+  const long rows = (long)total_q * num_q_heads;
+  const int n_hgroups = num_q_heads >> column_shift(num_q_heads / num_kv_heads);
+  const int kvs = cross_pieces(rows, estimate_wg128(rows, batch, n_hgroups), max_kv_len);
+  const size_t pieces = kvs > 1 ? (size_t)rows * kvs * (head_dim + 2) * sizeof(float) : 0;
+  const size_t few = decode_multi_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim);
+  return pieces > few ? pieces : few;
+}
+
+int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens, const int32_t *block_table,
+                 int batch, int max_pages, int total_q, int max_q_len, int max_kv_len, int num_q_heads, float scale, void *workspace,
+                 size_t workspace_bytes, hipStream_t stream) {
+  {
+    DecodeArgs d;
+    dim3 wgs;
+    int pieces = 0;
+    const int tiles = plan_decode_cross(d, c, q, out, cu_q, kv_lens, block_table, batch, max_pages, max_q_len, max_kv_len, num_q_heads, scale,
+                                        workspace, workspace_bytes, &wgs, &pieces);
+    if (tiles == 1) return c.head_dim == 128 ? launch_cross_stream<128, 1>(d, wgs, pieces, stream) : launch_cross_stream<64, 1>(d, wgs, pieces, stream);
+    if (tiles == 2) return c.head_dim == 128 ? launch_cross_stream<128, 2>(d, wgs, pieces, stream) : launch_cross_stream<64, 2>(d, wgs, pieces, stream);
+  }
+  CrossArgs a = {};
+  a.k_pages = (const char *)c.k_pages;
+  a.v_pages = (const char *)c.v_pages;
+  a.q = (const char *)q;
+  a.out = (char *)out;
+  a.cu_q = cu_q;
+  a.ctx_lens = kv_lens;
+  a.block_table = block_table;
+  a.max_pages = max_pages;
+  a.num_pages = c.num_pages;
+  a.Hq = num_q_heads;
+  a.Hkv = c.num_kv_heads;
+  a.gshift = column_shift(num_q_heads / c.num_kv_heads);
+  a.n_hgroups = num_q_heads >> a.gshift;
+  a.sl2e = scale * 1.44269504088896340736f;
+  a.tau = 8.0f / a.sl2e;
+  a.batch = batch;
+  a.total_q = total_q;
+  const long rows = (long)total_q * num_q_heads, streams = (long)batch * a.n_hgroups, wg128 = estimate_wg128(rows, batch, a.n_hgroups);
+  int kvs = workspace ? cross_pieces(rows, wg128, max_kv_len) : 1;
+  const size_t fit = workspace_bytes / ((size_t)rows * (c.head_dim + 2) * sizeof(float));
+  if ((size_t)kvs > fit) kvs = fit > 1 ? (int)fit : 1;
+  a.kv_splits = kvs;
+  a.part_o = (float *)workspace;
+  a.part_ml = a.part_o + (size_t)rows * kvs * c.head_dim;
+  // Key ranges of different lengths: longest first.
+  a.ranked = batch >= 2 && batch <= 64 * kRankSlots;
+  a.rank_shift = 6;
+  while (a.rank_shift < 24 && (((long)max_kv_len + max_q_len) >> a.rank_shift) > 63) ++a.rank_shift;
+  const bool split = kvs > 1 || (is_small_grid(wg128) && !whole_tiles_pay(rows, streams, max_kv_len));
+  const int rc = c.head_dim == 128 ? launch_cross_d<128>(a, split, batch, max_q_len, stream) : launch_cross_d<64>(a, split, batch, max_q_len, stream);
+  if (rc != SP_OK || kvs == 1) return rc;
+  return launch_combine(a.part_o, a.part_ml, out, rows, kvs, c.head_dim, stream, cu_q, batch, num_q_heads);
+}
+
+}  // namespace sp

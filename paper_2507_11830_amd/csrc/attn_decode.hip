@@ -784,6 +784,9 @@ static int multi_shape(int batch, int max_q_len, int num_q_heads, int num_kv_hea
   return a->geff <= 4 || (long)batch * a->n_hgroups <= 32 ? 2 : 0;
 }
 
+static void set_chunk_args(DecodeArgs &a, const sp_cache_desc &c, const void *k_new, const void *v_new, const void *q,
+                           const int32_t *cu_q, const int32_t *ctx_lens, const int32_t *block_table, int max_pages, float scale);
+
 size_t decode_multi_workspace_bytes(int batch, int total_q, int max_q_len, int max_kv_len, int num_q_heads,
                                     int num_kv_heads, int head_dim) {
   DecodeArgs a;
@@ -792,6 +795,17 @@ size_t decode_multi_workspace_bytes(int batch, int total_q, int max_q_len, int m
   const int chunk = pick_chunk(batch, num_q_heads, max_kv_len, max_q_len);
   const size_t nsplit = (size_t)(max_kv_len + chunk - 1) / chunk;
   return (size_t)total_q * num_q_heads * nsplit * (head_dim + 2) * sizeof(float);
+}
+
+int plan_decode_cross(DecodeArgs &a, const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens,
+                      const int32_t *block_table, int batch, int max_pages, int max_q_len, int max_kv_len, int num_q_heads, float scale,
+                      void *workspace, size_t workspace_bytes, dim3 *grid, int *pieces) {
+  const int tiles = multi_shape(batch, max_q_len, num_q_heads, c.num_kv_heads, &a);
+  if (tiles == 0 || max_kv_len <= 0 || max_pages <= 0) return 0;
+  a.route_cap = 0;
+  set_chunk_args(a, c, nullptr, nullptr, q, cu_q, kv_lens, block_table, max_pages, scale);
+  a.out = (char *)out;
+  return plan_decode_stream(a, batch, max_q_len, tiles, max_kv_len, c.head_dim, workspace, workspace_bytes, 0, true, grid, pieces) ? 0 : tiles;
 }
 
 // Mixed batches (sequences with a few query tokens next to sequences with long chunks, the usual

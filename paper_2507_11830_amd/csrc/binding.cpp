@@ -9,6 +9,8 @@
 #include <pthread.h>
 #include <stdint.h>
 
+#include <vector>
+
 #include "shiftattn.h"
 
 namespace {
@@ -17,11 +19,17 @@ struct Entry {
   const char *name;
   void *fn;
 };
-enum { kAppend, kPrefill, kChunkStep, kDecode, kDecodeStatic, kDecodeStep, kEntries };
+enum {
+  kAppend, kPrefill, kChunkStep, kDecode, kDecodeStatic, kDecodeStep, kRequired,  // a library without the others can be bound, and called for these
+  kCross = kRequired, kNormRope, kReserve, kFork, kRelease, kCompact, kCopy, kEntries
+};
 Entry entries[kEntries] = {{"sp_kv_append", nullptr},   {"sp_attn_prefill", nullptr},       {"sp_chunk_step", nullptr},
-                           {"sp_attn_decode", nullptr}, {"sp_attn_decode_static", nullptr}, {"sp_decode_step", nullptr}};
-PyObject *s_data_ptr, *s_shape, *s_numel, *s_element_size, *s_cuda_stream, *s_desc, *s_value, *s_as_parameter;
-PyObject *argument_error, *c_int32, *desc_type;    // ctypes.ArgumentError, ctypes.c_int32, sp_cache_desc
+                           {"sp_attn_decode", nullptr}, {"sp_attn_decode_static", nullptr}, {"sp_decode_step", nullptr},
+                           {"sp_attn_cross", nullptr},  {"sp_norm_rope_append", nullptr},   {"sp_pages_reserve", nullptr},
+                           {"sp_pages_fork", nullptr},  {"sp_pages_release", nullptr},      {"sp_pages_compact", nullptr},
+                           {"sp_pages_copy", nullptr}};
+PyObject *s_stride, *s_data_ptr, *s_shape, *s_numel, *s_element_size, *s_cuda_stream, *s_desc, *s_value, *s_as_parameter;
+PyObject *argument_error, *c_int32, *desc_type, *table_type;  // ctypes.ArgumentError, ctypes.c_int32, sp_cache_desc, sp_page_table
 PyObject *get_device, *get_stream, *first_stream;  // torch's raw accessors; the public one, for the first call of the process
 bool stream_used = false;  // the public accessor has been called in this process
 
@@ -124,27 +132,29 @@ bool scale_of(PyObject *o, float *out) {
   return true;
 }
 
-struct Desc {  // cache.desc, a ctypes structure: its memory
+struct Desc {  // cache.desc or table.desc, a ctypes structure: its memory
   Py_buffer view;
   bool held = false;
-  bool take(PyObject *cache) {
+  bool take(PyObject *cache, PyObject *type = desc_type, const char *otherwise = "cache.desc is not a cache descriptor") {
     PyObject *d = PyObject_GetAttr(cache, s_desc);
     if (!d) return false;
-    const int is = PyObject_IsInstance(d, desc_type);
+    const int is = type ? PyObject_IsInstance(d, type) : 0;
     if (is > 0) held = PyObject_GetBuffer(d, &view, PyBUF_SIMPLE) == 0;
-    else if (is == 0) PyErr_SetString(argument_error, "cache.desc is not a cache descriptor");
+    else if (is == 0) PyErr_SetString(argument_error, otherwise);
     Py_DECREF(d);
     return held;
   }
+  bool take_table(PyObject *table) { return take(table, table_type, "table.desc is not a page table"); }
   const sp_cache_desc *get() const { return (const sp_cache_desc *)view.buf; }
+  const sp_page_table *table() const { return (const sp_page_table *)view.buf; }
   ~Desc() {
     if (held) PyBuffer_Release(&view);
   }
 };
 
-bool count(const char *name, Py_ssize_t have, Py_ssize_t want) {
-  if (have == want && entries[0].fn) return true;
-  PyErr_Format(PyExc_TypeError, entries[0].fn ? "%s: %zd arguments, not %zd" : "%s: the library is not bound", name, want, have);
+bool count(const char *name, Py_ssize_t have, Py_ssize_t want, int entry = kAppend) {
+  if (have == want && entries[entry].fn) return true;
+  PyErr_Format(PyExc_TypeError, entries[entry].fn ? "%s: %zd arguments, not %zd" : "%s: the library is not bound", name, want, have);
   return false;
 }
 
@@ -264,20 +274,225 @@ PyObject *decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// bind(addresses, ArgumentError, c_int32, sp_cache_desc, get_device, get_stream, first_stream): addresses maps the C-ABI names to the
-// loaded library's functions
+// (cache, q, out, cu_seqlens_q, kv_lens, block_table, max_q_len, max_kv_len, scale, workspace, stream)
+PyObject *attn_cross(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Desc desc;
+  void *p[5], *ws, *stream;
+  int32_t table[2], q[2], max_q, max_kv;
+  float scale;
+  size_t ws_bytes;
+  if (!count("attn_cross", n, 11, kCross) || !dims(a[5], table, 2, true) || !dims(a[1], q, 2, false) || !bytes_of(a[9], &ws_bytes) || !desc.take(a[0]))
+    return nullptr;
+  for (int i = 0; i < 5; ++i)
+    if (!pointer(a[1 + i], p + i)) return nullptr;
+  if (!scale_of(a[8], &scale) || !pointer(a[9], &ws) || !stream_of(a[10], &stream) || !int32(a[6], &max_q) || !int32(a[7], &max_kv)) return nullptr;
+  return finish([&] {
+    return ((decltype(&sp_attn_cross))entries[kCross].fn)(desc.get(), p[0], p[1], (const int32_t *)p[2], (const int32_t *)p[3],
+                                                          (const int32_t *)p[4], table[0], table[1], q[0], max_q, max_kv, q[1], scale, ws, ws_bytes,
+                                                          stream);
+  });
+}
+
+// The heads and the distance between the tokens of a tensor [tokens][heads][head_dim] whose rows of a token are contiguous.  tokens: those
+// of the tensors before it, or -1.
+bool rows_of(PyObject *t, const char *name, int32_t head_dim, int32_t *tokens, int32_t *heads, int64_t *stride) {
+  int32_t size[3];
+  if (!dims(t, size, 3, true)) return false;
+  PyObject *s = PyObject_CallMethodNoArgs(t, s_stride);
+  PyObject *fast = s ? PySequence_Fast(s, "stride is not a sequence") : nullptr;
+  Py_XDECREF(s);
+  if (!fast) return false;
+  int64_t step[3] = {0, 0, 0};
+  if (PySequence_Fast_GET_SIZE(fast) == 3)
+    for (int i = 0; i < 3; ++i) step[i] = PyLong_AsLongLong(PySequence_Fast_GET_ITEM(fast, i));
+  Py_DECREF(fast);
+  if (PyErr_Occurred()) return false;
+  const int64_t row = (int64_t)size[1] * size[2];
+  if (size[2] != head_dim || (*tokens >= 0 && size[0] != *tokens) || (size[0] > 0 && (step[2] != 1 || (size[1] > 1 && step[1] != size[2])))) {
+    PyErr_Format(PyExc_ValueError, "%s: [tokens][heads][%d] with contiguous heads, as many tokens as the others", name, (int)head_dim);
+    return false;
+  }
+  *tokens = size[0];
+  *heads = size[1];
+  *stride = size[0] <= 1 ? row : step[0];
+  return true;
+}
+
+// (cache, q, k, v, q_out, cu_seqlens_new, ctx_lens, block_table, q_weight, k_weight, eps, cos_sin, interleaved, positions, stream)
+PyObject *norm_rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Desc desc;
+  void *p[9], *cos_sin, *positions, *stream;
+  int32_t table[2] = {0, 0}, tokens = -1, hq = 0, hk = 0, hv = 0, angles[2] = {0, 0};
+  int64_t strides[3] = {0, 0, 0};
+  float eps;
+  if (!count("norm_rope_append", n, 15, kNormRope) || !desc.take(a[0])) return nullptr;
+  const int32_t d = desc.get()->head_dim, hkv = desc.get()->num_kv_heads;
+  if (a[7] == Py_None ? !dims(a[6], table, 1, false) : !dims(a[7], table, 2, true)) return nullptr;
+  if (a[1] != Py_None) {
+    int32_t ho;
+    int64_t so;
+    if (!rows_of(a[1], "q", d, &tokens, &hq, strides) || !rows_of(a[4], "q_out", d, &tokens, &ho, &so)) return nullptr;
+    if (ho != hq || so != (int64_t)hq * d) {
+      PyErr_SetString(PyExc_ValueError, "q_out: contiguous, with the heads of q");
+      return nullptr;
+    }
+  }
+  if (a[2] != Py_None && !rows_of(a[2], "k", d, &tokens, &hk, strides + 1)) return nullptr;
+  if (a[3] != Py_None && !rows_of(a[3], "v", d, &tokens, &hv, strides + 2)) return nullptr;
+  if ((a[2] != Py_None && hk != hkv) || (a[3] != Py_None && hv != hkv)) {
+    PyErr_Format(PyExc_ValueError, "k and v: the cache has %d heads", (int)hkv);
+    return nullptr;
+  }
+  for (int i = 0; i < 9; ++i)
+    if (!pointer(a[1 + i], p + i)) return nullptr;
+  if (!scale_of(a[10], &eps) || !pointer(a[11], &cos_sin) || !pointer(a[13], &positions) || !stream_of(a[14], &stream)) return nullptr;
+  if (a[11] != Py_None && !dims(a[11], angles, 2, true)) return nullptr;
+  const int interleaved = PyObject_IsTrue(a[12]);
+  if (interleaved < 0) return nullptr;
+  const sp_rope_desc rope = {(const float *)cos_sin, angles[0], angles[1], interleaved};
+  return finish([&] {
+    return ((decltype(&sp_norm_rope_append))entries[kNormRope].fn)(
+        desc.get(), p[0], p[1], p[2], strides[0], strides[1], strides[2], p[3], p[7], p[8], eps, a[11] == Py_None ? nullptr : &rope,
+        (const int32_t *)positions, (const int32_t *)p[4], (const int32_t *)p[5], (const int32_t *)p[6], table[0], table[1], tokens < 0 ? 0 : tokens, hq,
+        stream);
+  });
+}
+
+// (table, rows, new_lens, shortfall, workspace, stream)
+PyObject *pages_reserve(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Desc desc;
+  void *p[4], *stream;
+  int32_t entries_n, more;
+  size_t ws_bytes;
+  if (!count("pages_reserve", n, 6, kReserve) || !dims(a[1], &entries_n, 1, true) || !dims(a[2], &more, 1, true) || !bytes_of(a[4], &ws_bytes) ||
+      !desc.take_table(a[0]))
+    return nullptr;
+  if (more != entries_n) return PyErr_Format(PyExc_ValueError, "rows and new_lens: %d and %d entries", (int)entries_n, (int)more);
+  for (int i = 0; i < 4; ++i)
+    if (!pointer(a[1 + i], p + i)) return nullptr;
+  if (!stream_of(a[5], &stream)) return nullptr;
+  return finish([&] {
+    return ((decltype(&sp_pages_reserve))entries[kReserve].fn)(desc.table(), (const int32_t *)p[0], (const int32_t *)p[1], entries_n, (int32_t *)p[2],
+                                                               p[3], ws_bytes, stream);
+  });
+}
+
+// (table, parents, children, copy_src, copy_dst, copy_rows, shortfall, workspace, stream)
+PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Desc desc;
+  void *p[7], *stream;
+  int32_t sizes[5];
+  size_t ws_bytes;
+  if (!count("pages_fork", n, 9, kFork)) return nullptr;
+  for (int i = 0; i < 5; ++i) {
+    if (!dims(a[1 + i], sizes + i, 1, true)) return nullptr;
+    if (sizes[i] != sizes[0]) return PyErr_Format(PyExc_ValueError, "%d parents, and an array of %d entries", (int)sizes[0], (int)sizes[i]);
+  }
+  if (!bytes_of(a[7], &ws_bytes) || !desc.take_table(a[0])) return nullptr;
+  for (int i = 0; i < 7; ++i)
+    if (!pointer(a[1 + i], p + i)) return nullptr;
+  if (!stream_of(a[8], &stream)) return nullptr;
+  return finish([&] {
+    return ((decltype(&sp_pages_fork))entries[kFork].fn)(desc.table(), (const int32_t *)p[0], (const int32_t *)p[1], sizes[0], (int32_t *)p[2],
+                                                         (int32_t *)p[3], (int32_t *)p[4], (int32_t *)p[5], p[6], ws_bytes, stream);
+  });
+}
+
+// (table, rows, keep_lens, stream)
+PyObject *pages_release(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Desc desc;
+  void *p[2], *stream;
+  int32_t entries_n, more;
+  if (!count("pages_release", n, 4, kRelease) || !dims(a[1], &entries_n, 1, true) || !desc.take_table(a[0])) return nullptr;
+  if (a[2] != Py_None) {
+    if (!dims(a[2], &more, 1, true)) return nullptr;
+    if (more != entries_n) return PyErr_Format(PyExc_ValueError, "rows and keep_lens: %d and %d entries", (int)entries_n, (int)more);
+  }
+  if (!pointer(a[1], p) || !pointer(a[2], p + 1) || !stream_of(a[3], &stream)) return nullptr;
+  return finish([&] {
+    return ((decltype(&sp_pages_release))entries[kRelease].fn)(desc.table(), (const int32_t *)p[0], (const int32_t *)p[1], entries_n, stream);
+  });
+}
+
+// (table, new_block_table, new_ref_counts, move_src, move_dst, moved, workspace, stream)
+PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Desc desc;
+  void *p[6], *stream;
+  int32_t table[2], sizes[4];
+  size_t ws_bytes;
+  if (!count("pages_compact", n, 8, kCompact) || !dims(a[1], table, 2, true) || !bytes_of(a[6], &ws_bytes) || !desc.take_table(a[0])) return nullptr;
+  for (int i = 0; i < 4; ++i)
+    if (!dims(a[2 + i], sizes + i, 1, true)) return nullptr;
+  const sp_page_table *t = desc.table();
+  if (table[0] != t->num_rows || table[1] != t->max_pages_per_seq || sizes[0] != t->num_pages || sizes[1] < t->num_pages / 2 ||
+      sizes[2] < t->num_pages / 2 || sizes[3] < 2) {
+    PyErr_SetString(PyExc_ValueError, "pages_compact: new arrays of the table's sizes, num_pages / 2 moves and 2 counts");
+    return nullptr;
+  }
+  for (int i = 0; i < 6; ++i)
+    if (!pointer(a[1 + i], p + i)) return nullptr;
+  if (!stream_of(a[7], &stream)) return nullptr;
+  return finish([&] {
+    return ((decltype(&sp_pages_compact))entries[kCompact].fn)(t, (int32_t *)p[0], (int32_t *)p[1], (int32_t *)p[2], (int32_t *)p[3], (int32_t *)p[4],
+                                                               p[5], ws_bytes, stream);
+  });
+}
+
+// (caches, src, dst, rows, count, stream): caches is a sequence
+PyObject *pages_copy(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  void *p[4], *stream;
+  int32_t pairs, more;
+  if (!count("pages_copy", n, 6, kCopy) || !dims(a[1], &pairs, 1, true)) return nullptr;
+  for (int i = 2; i < 4; ++i) {
+    if (i == 3 && a[3] == Py_None) continue;
+    if (!dims(a[i], &more, 1, true)) return nullptr;
+    if (more != pairs) return PyErr_Format(PyExc_ValueError, "%d sources, and an array of %d entries", (int)pairs, (int)more);
+  }
+  PyObject *fast = PySequence_Fast(a[0], "caches is not a sequence");
+  if (!fast) return nullptr;
+  const Py_ssize_t m = PySequence_Fast_GET_SIZE(fast);
+  std::vector<sp_cache_desc> caches;
+  bool ok = m <= INT32_MAX;
+  try {
+    caches.reserve(m);
+  } catch (...) {
+    ok = false;
+  }
+  if (!ok) PyErr_NoMemory();
+  for (Py_ssize_t i = 0; ok && i < m && i < PySequence_Fast_GET_SIZE(fast); ++i) {
+    Desc desc;
+    ok = desc.take(PySequence_Fast_GET_ITEM(fast, i));
+    if (ok) caches.push_back(*desc.get());
+  }
+  Py_DECREF(fast);
+  if (!ok) return nullptr;
+  for (int i = 0; i < 4; ++i)
+    if (!pointer(a[1 + i], p + i)) return nullptr;
+  if (!stream_of(a[5], &stream)) return nullptr;
+  return finish([&] {
+    return ((decltype(&sp_pages_copy))entries[kCopy].fn)(caches.data(), (int32_t)caches.size(), (const int32_t *)p[0], (const int32_t *)p[1],
+                                                         (const int32_t *)p[2], (const int32_t *)p[3], pairs, stream);
+  });
+}
+
+// bind(addresses, ArgumentError, c_int32, sp_cache_desc, get_device, get_stream, first_stream[, sp_page_table]): addresses maps the C-ABI
+// names to the loaded library's functions
 PyObject *bind(PyObject *, PyObject *args) {
-  PyObject *table, *values[6];
-  if (!PyArg_ParseTuple(args, "O!OOOOOO", &PyDict_Type, &table, values, values + 1, values + 2, values + 3, values + 4, values + 5)) return nullptr;
+  PyObject *table, *values[7] = {};
+  if (!PyArg_ParseTuple(args, "O!OOOOOO|O", &PyDict_Type, &table, values, values + 1, values + 2, values + 3, values + 4, values + 5, values + 6))
+    return nullptr;
   void *fn[kEntries];
   for (int i = 0; i < kEntries; ++i) {
     PyObject *v = PyDict_GetItemString(table, entries[i].name);
+    fn[i] = nullptr;
+    if (!v && i >= kRequired) continue;
     if (!v) return PyErr_Format(PyExc_KeyError, "%s", entries[i].name);
     fn[i] = PyLong_AsVoidPtr(v);
     if (!fn[i]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "%s is NULL", entries[i].name);
   }
-  PyObject **slots[6] = {&argument_error, &c_int32, &desc_type, &get_device, &get_stream, &first_stream};
-  for (int i = 0; i < 6; ++i) {
+  PyObject **slots[7] = {&argument_error, &c_int32, &desc_type, &get_device, &get_stream, &first_stream, &table_type};
+  for (int i = 0; i < 7; ++i) {
+    if (!values[i]) continue;
     Py_INCREF(values[i]);
     Py_XSETREF(*slots[i], values[i]);
   }
@@ -287,7 +502,8 @@ PyObject *bind(PyObject *, PyObject *args) {
 
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, FAST(kv_append), FAST(attn_prefill), FAST(chunk_step), FAST(attn_decode),
-                         FAST(attn_decode_static), FAST(decode_step), {nullptr, nullptr, 0, nullptr}};
+                         FAST(attn_decode_static), FAST(decode_step), FAST(attn_cross), FAST(norm_rope_append), FAST(pages_reserve),
+                         FAST(pages_fork), FAST(pages_release), FAST(pages_compact), FAST(pages_copy), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -296,7 +512,7 @@ PyMODINIT_FUNC PyInit__binding(void) {
   struct {
     PyObject **slot;
     const char *text;
-  } names[] = {{&s_data_ptr, "data_ptr"},       {&s_shape, "shape"}, {&s_numel, "numel"}, {&s_element_size, "element_size"},
+  } names[] = {{&s_stride, "stride"},           {&s_data_ptr, "data_ptr"},       {&s_shape, "shape"}, {&s_numel, "numel"}, {&s_element_size, "element_size"},
                {&s_cuda_stream, "cuda_stream"}, {&s_desc, "desc"},   {&s_value, "value"},   {&s_as_parameter, "_as_parameter_"}};
   // In a forked child torch's device state is unusable: the public accessor says so, the raw ones go on.
   static bool registered = false;

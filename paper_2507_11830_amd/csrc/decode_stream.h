@@ -22,7 +22,8 @@ __device__ __forceinline__ int load_pages(const DecodeArgs &a, int seq, int p0, 
 
 // Key blocks [p0, p1) of one row, by the whole workgroup.  pages: load_pages of the segment's first blocks.
 // whole: they are all of the row's, so the result is the output row; otherwise it goes to partial slot `slot`.
-template <int D, bool APPEND, bool MQ, int NT>
+// CROSS: all query tokens see all L keys (with ctx = L - query tokens).
+template <int D, bool APPEND, bool MQ, int NT, bool CROSS = false>
 __device__ __forceinline__ void row_segment(const DecodeArgs &a, lds_char *smem, int lane, int w, int seq, int hg, int L, int ctx,
                                             int tok_base, int p0, int p1, int pages, bool whole, int slot) {
   using G = TileGeom<D>;
@@ -52,7 +53,7 @@ __device__ __forceinline__ void row_segment(const DecodeArgs &a, lds_char *smem,
   for (int nt = 0; nt < NT; ++nt) {
     const int t = nt * a.q_cap + t0;  // tile nt holds the tokens nt * q_cap .. (nt + 1) * q_cap - 1
     col_valid[nt] = MQ ? t0 < a.q_cap && t < qn : col < a.geff;
-    lim_col[nt] = MQ ? (col_valid[nt] ? ctx + t + 1 : L) : 0;
+    lim_col[nt] = MQ ? (col_valid[nt] && !CROSS ? ctx + t + 1 : L) : 0;
     const char *qrow = a.q + ((long)(tok_base + t) * a.Hq + head0 + h_col) * (D * 2);
 #pragma unroll
     for (int s = 0; s < G::kDSteps; ++s) {
@@ -219,7 +220,7 @@ __device__ __forceinline__ void row_segment(const DecodeArgs &a, lds_char *smem,
       }
       wave_lds_fence();
     }
-    attend_block<D, MQ, NT>(sbk, sbv, kofs, vofs, qreg, o, m, l, base, kv1, ctx + 1, lim_col, half, a.sl2e, a.tau, L <= 256, [] {});
+    attend_block<D, MQ, NT>(sbk, sbv, kofs, vofs, qreg, o, m, l, base, kv1, CROSS ? L : ctx + 1, lim_col, half, a.sl2e, a.tau, L <= 256, [] {});
   }
 
   // ---- merge of the four waves' states: every wave leaves its o, m and l in LDS (rows padded by 16
@@ -283,8 +284,21 @@ __device__ __forceinline__ void zero_row(const DecodeArgs &a, int seq, int hg) {
   for (int i = threadIdx.x; i < a.geff * (D / 8); i += 64 * kWaves) *reinterpret_cast<u32x4 *>(dst + 16 * i) = (u32x4){0, 0, 0, 0};
 }
 
+// out rows of a chunk without keys (CROSS)
+template <int D>
+__device__ __forceinline__ void zero_chunk(const DecodeArgs &a, int tok, int qn, int hg) {
+  const int per = a.geff * (D / 8), n = min(qn, a.q_max);
+  for (int t = 0; t < n; ++t) {
+    char *dst = a.out + ((long)(tok + t) * a.Hq + hg * a.geff) * (D * 2);
+    for (int i = threadIdx.x; i < per; i += 64 * kWaves) *reinterpret_cast<u32x4 *>(dst + 16 * i) = (u32x4){0, 0, 0, 0};
+  }
+}
+
+// Keys of a sequence (CROSS), none beyond its row of the block table.
+__device__ __forceinline__ int cross_keys(const DecodeArgs &a, int kv_len) { return (int)min((long)max(kv_len, 0), (long)a.max_pages * kPage); }
+
 // Share number wg of the batch's rows, by kWaves waves (further threads of the workgroup have ended).
-template <int D, bool APPEND, bool MQ, int NT>
+template <int D, bool APPEND, bool MQ, int NT, bool CROSS = false>
 __device__ __forceinline__ void decode_share(const DecodeArgs &a, lds_char *smem, int lane, int w, int wg) {
   constexpr int RING = kWaves * 2 * 2 * 32 * D * 2;
   // Blocks of a sequence's row plus the row's fixed cost; 0 for a sequence that has no output row here.
@@ -305,8 +319,8 @@ __device__ __forceinline__ void decode_share(const DecodeArgs &a, lds_char *smem
       if (MQ) {
         const int tok = a.cu_q[s], ctx = a.ctx_lens[s];
         qn = a.cu_q[s + 1] - tok;
-        len = ctx + qn;
-        s_ctx[s] = ctx;
+        len = CROSS ? cross_keys(a, ctx) : ctx + qn;
+        s_ctx[s] = CROSS ? len - qn : ctx;
         s_tok[s] = tok;
       } else {
         len = a.seq_lens[s];
@@ -344,6 +358,7 @@ __device__ __forceinline__ void decode_share(const DecodeArgs &a, lds_char *smem
     const int row = seq * a.n_hgroups + hg;
     if (first == last) {
       if (!MQ && row0 >= lo) zero_row<D>(a, seq, hg);
+      if (CROSS && row0 >= lo) zero_chunk<D>(a, tok, L - ctx, hg);
       if (row0 >= lo && threadIdx.x == 0) *reinterpret_cast<u32x2 *>(a.row_tab + 2 * (long)row) = (u32x2){0, 1};
     } else if (p1 > p0) {
       const bool whole = p0 == 0 && p1 == v - kRowCost;
@@ -351,7 +366,7 @@ __device__ __forceinline__ void decode_share(const DecodeArgs &a, lds_char *smem
         const uint32_t pieces = whole ? 1 : (uint32_t)share_pieces(last, share, wg);
         *reinterpret_cast<u32x2 *>(a.row_tab + 2 * (long)row) = (u32x2){(uint32_t)(wg + row), pieces};
       }
-      row_segment<D, APPEND, MQ, NT>(a, smem, lane, w, seq, hg, L, ctx, tok, p0, p1, load_pages(a, seq, p0, 0, w, lane), whole, wg + row);
+      row_segment<D, APPEND, MQ, NT, CROSS>(a, smem, lane, w, seq, hg, L, ctx, tok, p0, p1, load_pages(a, seq, p0, 0, w, lane), whole, wg + row);
     }
     if (last >= hi) return;
     if (p1 > p0) __syncthreads();  // the next segment's loads go where this one's states are

@@ -1,0 +1,469 @@
+// Pages of a cache, kept on the device (sp_pages_*): reserve, fork, release, compact, and the copies that forks and compactions ask for.
+//
+// The state is one array, ref_counts, the number of block-table entries that hold a page; a page is free if it is 0.  There is no
+// list of free pages whose order would depend on history: a call that takes pages reads the counts once, into a bit set
+// (64 pages a word) and a sum per segment of kSegment pages, and the k-th page that it takes is the k-th free one.  That costs 4 bytes
+// per page of the pool, but nothing orders one workgroup of the scan behind another, every workgroup of the
+// second launch finds its pages by itself, and the result does not depend on timing.
+//
+// Launches: reserve and fork two (scan and plan; apply), compact three (scan; ranks; apply), release and copy one.  All but
+// the copy are bound by their chains of memory round trips, the copy by HBM.
+#include "sp_common.h"
+
+namespace sp {
+
+constexpr int kPageThreads = 256, kPageWaves = kPageThreads / 64;
+constexpr int kSegment = 4096;              // pages per workgroup of the scan
+constexpr int kSegWords = kSegment / 64;    // 64: one per lane
+
+template <typename T>
+static __device__ __forceinline__ T lane_prefix(T x) {  // inclusive sum over the lanes
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const T y = __shfl_up(x, d);
+    if ((int)(threadIdx.x & 63) >= d) x += y;
+  }
+  return x;
+}
+// Inclusive sum over the workgroup's threads, and the sum of all; wave_sums: kPageWaves values in LDS.
+template <typename T>
+static __device__ __forceinline__ T block_prefix(T x, T *wave_sums, T *total) {
+  const int w = threadIdx.x >> 6;
+  const T incl = lane_prefix(x);
+  __syncthreads();  // wave_sums may still be read
+  if ((threadIdx.x & 63) == 63) wave_sums[w] = incl;
+  __syncthreads();
+  T before = 0, all = 0;
+#pragma unroll
+  for (int u = 0; u < kPageWaves; ++u) {
+    before += u < w ? wave_sums[u] : 0;
+    all += wave_sums[u];
+  }
+  *total = all;
+  return before + incl;
+}
+
+__host__ __device__ __forceinline__ int pages_of(int tokens) { return tokens <= 0 ? 0 : (int)(((unsigned)tokens + kPage - 1) / kPage); }
+
+struct PagesArgs {
+  int32_t *refs, *table, *lens;
+  int num_pages, num_rows, max_pages, nseg;
+  uint64_t *free_bits;  // [nseg * kSegWords]
+  int32_t *seg_free;    // [nseg] free pages of a segment
+  // reserve, fork
+  const int32_t *a, *b;  // rows and new lengths; parents and children
+  int n;
+  int32_t *plan;   // [n + 1] pages that the entries before take
+  int32_t *sizes;  // [n] fork: the parent's tokens, -1 for a skipped entry; reserve: the row's pages to be, 0 for a skipped entry
+  int32_t *shortfall, *copy_src, *copy_dst, *copy_rows;
+  // compact
+  int32_t *new_table, *new_refs, *move_src, *move_dst, *moved;
+  int32_t *rank, *moved_refs;  // [num_pages] of holes and of pages that move; [num_pages / 2] counts of the latter
+};
+
+// Tokens of a row, none beyond what its table row holds.
+static __device__ __forceinline__ int row_tokens(const PagesArgs &p, int row) {
+  const long most = (long)p.max_pages * kPage;
+  const int len = p.lens[row];
+  return len < 0 ? 0 : len > most ? (int)most : len;
+}
+
+enum { kCompact, kReserve, kFork };
+
+// Workgroup s < nseg: the free pages of segment s.  Workgroup nseg: what every entry takes, and the sums of that before it.
+template <int OP>
+__global__ __launch_bounds__(kPageThreads) void pages_scan_kernel(PagesArgs p) {
+  __shared__ int wave_sums[kPageWaves];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  if ((int)blockIdx.x < p.nseg) {
+    constexpr int PER = kSegWords / kPageWaves;  // words of a wave
+    const long base = (long)blockIdx.x * kSegment + w * (PER * 64) + lane;
+    int refs[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) refs[i] = base + 64 * i < p.num_pages ? p.refs[base + 64 * i] : 1;
+    uint64_t mine = 0;
+    int free_pages = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint64_t bits = __builtin_amdgcn_ballot_w64(refs[i] <= 0);
+      free_pages += __builtin_popcountll(bits);
+      if (lane == i) mine = bits;
+    }
+    if (lane < PER) p.free_bits[(long)blockIdx.x * kSegWords + w * PER + lane] = mine;
+    if (lane == 0) wave_sums[w] = free_pages;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int sum = 0;
+#pragma unroll
+      for (int u = 0; u < kPageWaves; ++u) sum += wave_sums[u];
+      p.seg_free[blockIdx.x] = sum;
+    }
+    return;
+  }
+  if constexpr (OP != kCompact) {
+    __shared__ long long_sums[kPageWaves];
+    long before = 0;  // what the entries take together may pass 32 bits: then it is more than any pool has, and is stored as the most
+    for (long i0 = 0; i0 < p.n; i0 += kPageThreads) {
+      const long i = i0 + threadIdx.x;
+      long need = 0;
+      if (i < p.n) {
+        const int a = p.a[i], b = p.b[i];
+        int size = OP == kFork ? -1 : 0;
+        if (a >= 0 && a < p.num_rows) {
+          if (OP == kFork) {
+            if (b >= 0 && b < p.num_rows && p.lens[b] == 0) {
+              size = row_tokens(p, a);
+              need = size % kPage != 0;
+            }
+          } else if (pages_of(b) <= p.max_pages) {
+            size = pages_of(b);
+            need = max(size - pages_of(row_tokens(p, a)), 0);
+          }
+        }
+        p.sizes[i] = size;
+      }
+      long total;
+      const long incl = block_prefix(need, long_sums, &total);
+      if (i < p.n) p.plan[i + 1] = (int)min(before + incl, 0x7fffffffL);
+      before += total;
+    }
+    if (threadIdx.x == 0) p.plan[0] = 0;
+  }
+}
+
+// The free pages number first .. first + m - 1 of the pool in ascending order: take(k, page) for the k-th of them, k from 0, by any
+// thread.  c0: seg_free[threadIdx.x], 0 behind the last; by the whole workgroup.
+template <typename Take>
+static __device__ __forceinline__ void for_free_pages(const PagesArgs &p, int c0, int first, int m, int *wave_sums, int *seg_before, Take take) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int before = 0;
+  for (int s0 = 0; s0 < p.nseg && before < first + m; s0 += kPageThreads) {
+    const int s = s0 + threadIdx.x, c = s0 == 0 ? c0 : s < p.nseg ? p.seg_free[s] : 0;
+    int total;
+    const int incl = block_prefix(c, wave_sums, &total);
+    seg_before[threadIdx.x + 1] = before + incl;
+    if (threadIdx.x == 0) seg_before[0] = before;
+    __syncthreads();
+    if (before + total > first) {
+      // the segments that hold such pages: from the first that ends behind `first` on
+      int lo = 0, hi = kPageThreads;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (seg_before[mid + 1] > first) hi = mid;
+        else lo = mid + 1;
+      }
+      for (int q = lo + w; q < kPageThreads && s0 + q < p.nseg && seg_before[q] < first + m; q += kPageWaves) {
+        uint64_t bits = p.free_bits[(long)(s0 + q) * kSegWords + lane];
+        const int mine = __builtin_popcountll(bits);
+        int k = seg_before[q] + lane_prefix(mine) - mine - first;
+        const int page = (s0 + q) * kSegment + 64 * lane;
+        for (; bits != 0 && k < m; bits &= bits - 1, ++k)
+          if (k >= 0) take(k, page + __builtin_ctzll(bits));
+      }
+    }
+    before += total;
+  }
+}
+
+// Free pages of the pool; c0 as above.
+static __device__ __forceinline__ int all_free(const PagesArgs &p, int c0, int *wave_sums) {
+  int c = c0, total;
+  for (int s = threadIdx.x + kPageThreads; s < p.nseg; s += kPageThreads) c += p.seg_free[s];
+  block_prefix(c, wave_sums, &total);
+  return total;
+}
+
+// One workgroup per entry.
+template <int OP>
+__global__ __launch_bounds__(kPageThreads) void pages_take_kernel(PagesArgs p) {
+  __shared__ int wave_sums[kPageWaves], seg_before[kPageThreads + 1], s_old, s_page;
+  const int i = blockIdx.x, a = p.a[i], b = p.b[i];
+  const int first = p.plan[i], need = p.plan[i + 1] - first, wanted = p.plan[p.n], size = p.sizes[i];
+  const int c0 = (int)threadIdx.x < p.nseg ? p.seg_free[threadIdx.x] : 0;
+  const int missing = max(wanted - all_free(p, c0, wave_sums), 0);
+  if (i == 0 && threadIdx.x == 0) *p.shortfall = missing;
+  if constexpr (OP == kReserve) {
+    if (missing > 0 || size == 0) return;  // size > 0: a is a row of the table, and holds no more pages than b takes
+    // The entry that raises the length takes the pages: of several for one row each takes different ones.
+    if (threadIdx.x == 0) s_old = atomicMax(p.lens + a, b);
+    __syncthreads();
+    const int has = pages_of(s_old), m = min(size - has, need);
+    if (m <= 0) return;
+    int32_t *row = p.table + (long)a * p.max_pages + has;
+    for_free_pages(p, c0, first, m, wave_sums, seg_before, [&](int k, int page) __attribute__((always_inline)) {
+      row[k] = page;
+      p.refs[page] = 1;
+    });
+  } else {
+    bool taken = missing == 0 && size >= 0;
+    if (taken && size > 0) {
+      if (threadIdx.x == 0) s_old = atomicCAS(p.lens + b, 0, size);
+      __syncthreads();
+      taken = s_old == 0;
+    }
+    if (threadIdx.x == 0 && !(taken && need > 0)) {
+      p.copy_src[i] = p.copy_dst[i] = -1;
+      p.copy_rows[i] = 0;
+    }
+    if (!taken) return;
+    const int32_t *from = p.table + (long)a * p.max_pages;
+    int32_t *to = p.table + (long)b * p.max_pages;
+    const int full = size / kPage;
+    for (int c = threadIdx.x; c < full; c += kPageThreads) {
+      const int page = from[c];
+      to[c] = page;
+      if (page >= 0 && page < p.num_pages) atomicAdd(p.refs + page, 1);
+    }
+    if (need == 0) return;
+    for_free_pages(p, c0, first, 1, wave_sums, seg_before, [&](int, int page) __attribute__((always_inline)) { s_page = page; });
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      to[full] = s_page;
+      p.refs[s_page] = 1;
+      p.copy_src[i] = from[full];
+      p.copy_dst[i] = s_page;
+      p.copy_rows[i] = size % kPage;
+    }
+  }
+}
+
+// One workgroup per entry.  Lowering the length claims the pages behind it, so of several entries for one row each gives back
+// different ones.
+__global__ __launch_bounds__(kPageThreads) void pages_release_kernel(PagesArgs p, const int32_t *keep_lens) {
+  __shared__ int s_old;
+  const int row = p.a[blockIdx.x], keep = keep_lens ? max(keep_lens[blockIdx.x], 0) : 0;
+  if (row < 0 || row >= p.num_rows) return;
+  if (threadIdx.x == 0) s_old = atomicMin(p.lens + row, keep);
+  __syncthreads();
+  const int end = min(pages_of(s_old), p.max_pages);
+  int32_t *entries = p.table + (long)row * p.max_pages;
+  for (int c = pages_of(keep) + threadIdx.x; c < end; c += kPageThreads) {
+    const int page = entries[c];
+    entries[c] = -1;
+    if (page >= 0 && page < p.num_pages) atomicSub(p.refs + page, 1);
+  }
+}
+
+// Compaction, second launch: where the pages in use from U on go.  With M free pages below U, a free page below U has as many free
+// ones before it as its rank says, and a page in use from U on has its rank plus U - M pages in use before it.
+__global__ __launch_bounds__(kPageThreads) void pages_rank_kernel(PagesArgs p) {
+  __shared__ int wave_sums[kPageWaves], s_before[kSegWords], s_seg[2];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, seg = blockIdx.x;
+  const uint64_t my_bits = p.free_bits[(long)seg * kSegWords + lane];
+  int sum = 0, below = 0, total_free, before_seg;
+  for (int s = threadIdx.x; s < p.nseg; s += kPageThreads) {
+    const int c = p.seg_free[s];
+    sum += c;
+    below += s < seg ? c : 0;
+  }
+  block_prefix(sum, wave_sums, &total_free);
+  block_prefix(below, wave_sums, &before_seg);
+  const int used = p.num_pages - total_free, useg = used / kSegment;
+  // M: free pages below U
+  below = 0;
+  for (int s = threadIdx.x; s < useg; s += kPageThreads) below += p.seg_free[s];
+  if (useg < p.nseg && (int)threadIdx.x < kSegWords) {
+    const uint64_t bits = p.free_bits[(long)useg * kSegWords + threadIdx.x];
+    const int n = min(max(used - useg * kSegment - 64 * (int)threadIdx.x, 0), 64);  // its pages below U
+    below += __builtin_popcountll(n == 64 ? bits : bits & ((1ull << n) - 1));
+  }
+  int holes;
+  block_prefix(below, wave_sums, &holes);
+  if (seg == 0 && threadIdx.x == 0) {
+    p.moved[0] = holes;
+    p.moved[1] = used;
+  }
+  if (holes == 0) return;
+  if (w == 0) {
+    const int c = __builtin_popcountll(my_bits);
+    s_before[lane] = before_seg + lane_prefix(c) - c;
+  }
+  __syncthreads();
+  for (int k = w; k < kSegWords; k += kPageWaves) {
+    const long page = (long)seg * kSegment + 64 * k + lane;
+    const uint64_t bits = __shfl(my_bits, k);  // by all lanes
+    if (page >= p.num_pages) continue;
+    const int free_before = s_before[k] + __builtin_popcountll(bits & ((1ull << lane) - 1));
+    const bool is_free = (bits >> lane) & 1;
+    if (is_free && page < used) {
+      p.move_dst[free_before] = (int)page;
+      p.rank[page] = free_before;
+    } else if (!is_free && page >= used) {
+      const int r = (int)page - free_before - (used - holes);
+      p.move_src[r] = (int)page;
+      p.rank[page] = r;
+      p.moved_refs[r] = p.refs[page];
+    }
+  }
+}
+
+// Third launch: the counts (the first workgroups) and the rows.
+__global__ __launch_bounds__(kPageThreads) void pages_move_kernel(PagesArgs p, int count_groups) {
+  const int used = p.moved[1];
+  auto is_free = [&](long page) __attribute__((always_inline)) { return ((p.free_bits[page >> 6] >> (page & 63)) & 1) != 0; };
+  if ((int)blockIdx.x < count_groups) {
+    for (long page = (long)blockIdx.x * kPageThreads + threadIdx.x; page < p.num_pages; page += (long)count_groups * kPageThreads)
+      p.new_refs[page] = page >= used ? 0 : is_free(page) ? p.moved_refs[p.rank[page]] : p.refs[page];
+    return;
+  }
+  const int row = blockIdx.x - count_groups, n = pages_of(row_tokens(p, row));
+  for (int c = threadIdx.x; c < n; c += kPageThreads) {
+    const int page = p.table[(long)row * p.max_pages + c];
+    const bool moves = page >= used && page < p.num_pages && !is_free(page);
+    p.new_table[(long)row * p.max_pages + c] = moves ? p.move_dst[p.rank[page]] : page;
+  }
+}
+
+// ---- copies.  A wave copies kCopyChunks 16-byte chunks of one pool's page at a time: everything that it looks up is wave-uniform.
+constexpr int kCopyCaches = 64;  // caches of one launch: their pools are kernel arguments
+struct CopyArgs {
+  char *pools[2 * kCopyCaches];
+  const int32_t *src, *dst, *rows, *count;
+  int n, num_pools, num_pages, parts;  // parts: of a pool's page
+  int row_shift;                       // log2 of the 16-byte chunks of a row
+};
+
+template <int PER>  // chunks of a lane
+__global__ __launch_bounds__(kPageThreads) void pages_copy_kernel(CopyArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = a.count ? min(a.n, *a.count) : a.n;
+  const unsigned per_pair = (unsigned)(a.num_pools * a.parts);
+  const long units = (long)n * per_pair;
+  for (long u = (long)blockIdx.x * kPageWaves + w; u < units; u += (long)gridDim.x * kPageWaves) {
+    const int i = (int)(u / per_pair), rem = (int)(u - (long)i * per_pair), pool = rem / a.parts, part = rem - pool * a.parts;
+    const int src = a.src[i], dst = a.dst[i], rows = a.rows ? a.rows[i] : kPage;
+    if (src < 0 || src >= a.num_pages || dst < 0 || dst >= a.num_pages || src == dst) continue;
+    const size_t bytes = (size_t)a.parts * PER * 1024;
+    const u32x4 *from = (const u32x4 *)(a.pools[pool] + src * bytes);
+    u32x4 *to = (u32x4 *)(a.pools[pool] + dst * bytes);
+    u32x4 x[PER];
+    bool there[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int c = (part * PER + k) * 64 + lane;
+      there[k] = ((c >> a.row_shift) & (kPage - 1)) < rows;
+      if (there[k]) x[k] = from[c];
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (there[k]) to[(part * PER + k) * 64 + lane] = x[k];
+  }
+}
+
+// ---- host
+
+static size_t align16(size_t n) { return (n + 15) / 16 * 16; }
+static int segments(int num_pages) { return (int)(((long)num_pages + kSegment - 1) / kSegment); }
+
+size_t pages_workspace_bytes(int num_pages, int n) {
+  const size_t nseg = segments(num_pages), scan = nseg * kSegWords * 8 + align16(nseg * 4);
+  return scan + (n > 0 ? (size_t)align16(((size_t)n + 1) * 4) + (size_t)n * 4 : align16((size_t)num_pages * 4) + (size_t)(num_pages / 2) * 4);
+}
+
+static PagesArgs pages_args(const sp_page_table &t, void *workspace, int n) {
+  PagesArgs p = {};
+  p.refs = t.ref_counts;
+  p.table = t.block_table;
+  p.lens = t.seq_lens;
+  p.num_pages = t.num_pages;
+  p.num_rows = t.num_rows;
+  p.max_pages = t.max_pages_per_seq;
+  p.nseg = segments(t.num_pages);
+  p.n = n;
+  char *ws = (char *)workspace;
+  p.free_bits = (uint64_t *)ws;
+  ws += (size_t)p.nseg * kSegWords * 8;
+  p.seg_free = (int32_t *)ws;
+  ws += align16((size_t)p.nseg * 4);
+  if (n > 0) {
+    p.plan = (int32_t *)ws;
+    p.sizes = (int32_t *)(ws + align16(((size_t)n + 1) * 4));
+  } else {
+    p.rank = (int32_t *)ws;
+    p.moved_refs = (int32_t *)(ws + align16((size_t)t.num_pages * 4));
+  }
+  return p;
+}
+
+static int launched(const char *what) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SP_OK : fail(SP_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
+}
+
+int launch_pages_reserve(const sp_page_table &t, const int32_t *rows, const int32_t *new_lens, int n, int32_t *shortfall, void *workspace,
+                         hipStream_t stream) {
+  PagesArgs p = pages_args(t, workspace, n);
+  p.a = rows;
+  p.b = new_lens;
+  p.shortfall = shortfall;
+  hipLaunchKernelGGL(pages_scan_kernel<kReserve>, dim3(p.nseg + 1), dim3(kPageThreads), 0, stream, p);
+  hipLaunchKernelGGL(pages_take_kernel<kReserve>, dim3(n), dim3(kPageThreads), 0, stream, p);
+  return launched("sp_pages_reserve");
+}
+
+int launch_pages_fork(const sp_page_table &t, const int32_t *parents, const int32_t *children, int n, int32_t *copy_src, int32_t *copy_dst,
+                      int32_t *copy_rows, int32_t *shortfall, void *workspace, hipStream_t stream) {
+  PagesArgs p = pages_args(t, workspace, n);
+  p.a = parents;
+  p.b = children;
+  p.copy_src = copy_src;
+  p.copy_dst = copy_dst;
+  p.copy_rows = copy_rows;
+  p.shortfall = shortfall;
+  hipLaunchKernelGGL(pages_scan_kernel<kFork>, dim3(p.nseg + 1), dim3(kPageThreads), 0, stream, p);
+  hipLaunchKernelGGL(pages_take_kernel<kFork>, dim3(n), dim3(kPageThreads), 0, stream, p);
+  return launched("sp_pages_fork");
+}
+
+int launch_pages_release(const sp_page_table &t, const int32_t *rows, const int32_t *keep_lens, int n, hipStream_t stream) {
+  PagesArgs p = pages_args(t, nullptr, n);
+  p.a = rows;
+  hipLaunchKernelGGL(pages_release_kernel, dim3(n), dim3(kPageThreads), 0, stream, p, keep_lens);
+  return launched("sp_pages_release");
+}
+
+int launch_pages_compact(const sp_page_table &t, int32_t *new_block_table, int32_t *new_ref_counts, int32_t *move_src, int32_t *move_dst,
+                         int32_t *moved, void *workspace, hipStream_t stream) {
+  PagesArgs p = pages_args(t, workspace, 0);
+  p.new_table = new_block_table;
+  p.new_refs = new_ref_counts;
+  p.move_src = move_src;
+  p.move_dst = move_dst;
+  p.moved = moved;
+  const int count_groups = (int)min((long)1024, ((long)t.num_pages + kPageThreads - 1) / kPageThreads);
+  hipLaunchKernelGGL(pages_scan_kernel<kCompact>, dim3(p.nseg), dim3(kPageThreads), 0, stream, p);
+  hipLaunchKernelGGL(pages_rank_kernel, dim3(p.nseg), dim3(kPageThreads), 0, stream, p);
+  hipLaunchKernelGGL(pages_move_kernel, dim3((unsigned)count_groups + (unsigned)t.num_rows), dim3(kPageThreads), 0, stream, p, count_groups);
+  return launched("sp_pages_compact");
+}
+
+int launch_pages_copy(const sp_cache_desc *caches, int num_caches, const int32_t *src, const int32_t *dst, const int32_t *rows,
+                      const int32_t *count, int n, hipStream_t stream) {
+  const int row_chunks = caches[0].head_dim / 8, chunks = caches[0].num_kv_heads * kPage * row_chunks;  // a multiple of 128
+  const bool four = chunks % 256 == 0;
+  for (int c0 = 0; c0 < num_caches; c0 += kCopyCaches) {
+    CopyArgs a;
+    const int m = min(num_caches - c0, kCopyCaches);
+    for (int i = 0; i < kCopyCaches; ++i) {
+      a.pools[2 * i] = i < m ? (char *)caches[c0 + i].k_pages : nullptr;
+      a.pools[2 * i + 1] = i < m ? (char *)caches[c0 + i].v_pages : nullptr;
+    }
+    a.src = src;
+    a.dst = dst;
+    a.rows = rows;
+    a.count = count;
+    a.n = n;
+    a.num_pools = 2 * m;
+    a.num_pages = caches[0].num_pages;
+    a.parts = chunks / (four ? 256 : 128);
+    a.row_shift = row_chunks == 16 ? 4 : 3;
+    const long units = (long)n * a.num_pools * a.parts;
+    const unsigned groups = (unsigned)min((units + kPageWaves - 1) / kPageWaves, 256L * 8);
+    if (four) hipLaunchKernelGGL(pages_copy_kernel<4>, dim3(groups), dim3(kPageThreads), 0, stream, a);
+    else hipLaunchKernelGGL(pages_copy_kernel<2>, dim3(groups), dim3(kPageThreads), 0, stream, a);
+  }
+  return launched("sp_pages_copy");
+}
+
+}  // namespace sp

@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kSoloThreads, 3) void solo_prefill_kernel(Args a) {
   using G = TileGeom<D>;
   using Z = SwzTile<D>;
   using std::integral_constant;
-  constexpr bool FRESH = std::is_same<Args, FreshArgs>::value;
+  constexpr bool FRESH = std::is_same<Args, FreshArgs>::value, CROSS = std::is_same<Args, CrossArgs>::value;
   constexpr int WAVES = kSoloThreads / 64;
   constexpr int ROWB = D * 2;                     // bytes of one K or V row
   constexpr int TBYTES = KVT * ROWB;              // one tile in LDS
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kSoloThreads, 3) void solo_prefill_kernel(Args a) {
   if (!take_item<0, true>(a, 7, lane, &it)) return;
   const int tpt = kSoloCols >> a.gshift, tok0 = it.tile * tpt, q0 = it.q0, q_len = it.q_len, ctx = it.ctx, hg = it.hg;
   if (tok0 >= q_len) return;
-  const int kv_end = ctx + min(q_len, tok0 + tpt);
+  const int kv_end = CROSS ? cross_keys(a, ctx) : ctx + min(q_len, tok0 + tpt);
   const int kvh = (hg << a.gshift) / (a.Hq / a.Hkv);
   const int32_t *bt_row = a.block_table + (long)it.seq * a.max_pages;
 
@@ -69,9 +69,15 @@ __global__ __launch_bounds__(kSoloThreads, 3) void solo_prefill_kernel(Args a) {
   // ---- this lane's column and the resident Q^T operands
   const int C = w * 32 + col, token = tok0 + (C >> a.gshift);
   const bool valid = token < q_len;
-  const int lim = valid ? ctx + token + 1 : kv_end;  // a column without a query has scores of 0 and is not stored: any limit will do
-  const int wlim_min = min(ctx + tok0 + ((w * 32) >> a.gshift) + 1, kv_end);  // keys that all of the wave's columns see
+  const int lim = valid && !CROSS ? ctx + token + 1 : kv_end;  // a column without a query has scores of 0 and is not stored: any limit will do
+  const int wlim_min = CROSS ? kv_end : min(ctx + tok0 + ((w * 32) >> a.gshift) + 1, kv_end);  // keys that all of the wave's columns see
   const long out_off = ((long)(q0 + token) * a.Hq + ((hg << a.gshift) | (C & ((1 << a.gshift) - 1)))) * (D * 2);
+  if (CROSS && kv_end == 0) {  // no keys: rows of zeros
+    if (valid)
+#pragma unroll
+      for (int s = 0; s < G::kDSteps; ++s) *reinterpret_cast<u32x4 *>(a.out + out_off + 32 * s + 16 * half) = (u32x4){0, 0, 0, 0};
+    return;
+  }
   bf16x8 qreg[G::kDSteps];
 #pragma unroll
   for (int s = 0; s < G::kDSteps; ++s) {
@@ -248,7 +254,7 @@ __global__ __launch_bounds__(kSoloThreads, 3) void solo_prefill_kernel(Args a) {
   int pg = 0;        // page id of the next K load
   size_t pos_v = 0, pos_w = 0;  // where the pages of the next two V loads begin
   constexpr int kPreciseKeys = 256;
-  const bool precise = ctx + (it.tile & ~1) * tpt < kPreciseKeys;  // some rows of this tile or its neighbour, as with 256 columns, have at most that many keys
+  const bool precise = CROSS ? kv_end <= kPreciseKeys : ctx + (it.tile & ~1) * tpt < kPreciseKeys;  // some rows of this tile or its neighbour, as with 256 columns, have at most that many keys
   {
     int pg0 = 0, pg1 = 0;
     if (!FRESH || new_tile != 0) {

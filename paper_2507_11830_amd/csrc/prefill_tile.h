@@ -128,6 +128,10 @@ struct FreshArgs : PrefillArgs {
   const char *k_new, *v_new;  // bf16 [total_q][Hkv][D]
   int new_pages;              // pages that the new rows of a sequence reach into, at most
 };
+// CrossArgs: no mask (sp_attn_cross).  ctx_lens holds the number of keys, and every query sees all of them.
+struct CrossArgs : PrefillArgs {};
+// Keys of a sequence, none beyond its row of the block table.
+__device__ __forceinline__ int cross_keys(const PrefillArgs &a, int kv_len) { return (int)min((long)max(kv_len, 0), (long)a.max_pages * kPage); }
 constexpr int kFreshChunks = 1024;  // 16-byte chunks of K (and of V) in the rows of a query tile, at most: a few per thread
 
 __device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan_incl(x), 63); }
@@ -546,12 +550,13 @@ struct TileRows {
 //
 // Args = MixedArgs (attn_mixed.hip): the launch also holds workgroups of another kernel, behind the prefill ones.
 // Args = FreshArgs (attn_prefill_fresh.hip): the append happens here.
+// Args = CrossArgs (attn_cross.hip): every query sees all keys of its sequence.
 template <int D, int KVT, int PFD, bool SPLIT, bool PART, int CUT, typename Args = PrefillArgs>
 __global__ __launch_bounds__(512, 2) void prefill_kernel(Args a) {
   using G = TileGeom<D>;
   using Z = SwzTile<D>;
   constexpr int COLS = SPLIT ? 128 : 256, KB = KVT / 32;
-  constexpr bool FRESH = std::is_same<Args, FreshArgs>::value;
+  constexpr bool FRESH = std::is_same<Args, FreshArgs>::value, CROSS = std::is_same<Args, CrossArgs>::value;
   constexpr int ROWB = D * 2;               // bytes of one K or V row
   constexpr int TBYTES = KVT * ROWB;        // one tile in LDS
   constexpr int REGION = 4 * TBYTES;        // K[2] at 0 and TBYTES, V[2] at 2 and 3 TBYTES
@@ -568,7 +573,7 @@ __global__ __launch_bounds__(512, 2) void prefill_kernel(Args a) {
 #endif
 
   const int tid = threadIdx.x, lane = tid & 63;
-  if constexpr (!FRESH && !std::is_same<Args, PrefillArgs>::value) {
+  if constexpr (!FRESH && !CROSS && !std::is_same<Args, PrefillArgs>::value) {
     if (blockIdx.x >= a.first_other) {
       a.template run_other<D>(smem, lane);
       return;
@@ -585,7 +590,7 @@ __global__ __launch_bounds__(512, 2) void prefill_kernel(Args a) {
   const int tpt = COLS >> a.gshift;
   const int tok0 = tile * tpt;
   if (tok0 >= q_len) return;
-  const int kv_end = ctx + min(q_len, tok0 + tpt);
+  const int kv_end = CROSS ? cross_keys(a, ctx) : ctx + min(q_len, tok0 + tpt);
   const int kvh = (hg << a.gshift) / (a.Hq / a.Hkv);
   const int32_t *bt_row = a.block_table + (long)seq * a.max_pages;
   const int gmask = (1 << a.gshift) - 1;
@@ -612,8 +617,14 @@ __global__ __launch_bounds__(512, 2) void prefill_kernel(Args a) {
   const bool valid = token < q_len;
   // A column without a query (past the sequence's end) has scores of 0 and is not stored, so it takes any limit: with one of 1 key
   // its wave went through the mask in every tile instead of the last ones (1 x 5003 tokens, 8q/1kv: 77 -> 65 us).
-  const int lim = valid ? ctx + token + 1 : kv_end;
+  const int lim = valid && !CROSS ? ctx + token + 1 : kv_end;
   const long out_off = ((long)(q0 + token) * a.Hq + head) * (D * 2);
+  if (CROSS && !PART && kv_end == 0) {  // no keys: rows of zeros
+    if (valid && (!SPLIT || grp == 0))
+#pragma unroll
+      for (int s = 0; s < G::kDSteps; ++s) *reinterpret_cast<u32x4 *>(a.out + out_off + 32 * s + 16 * half) = (u32x4){0, 0, 0, 0};
+    return;
+  }
 #pragma unroll
   for (int s = 0; s < G::kDSteps; ++s) {
     if (valid) {
@@ -627,7 +638,7 @@ __global__ __launch_bounds__(512, 2) void prefill_kernel(Args a) {
   // Rows with at most kPreciseKeys keys get hi + lo weights (see pv_residual below); the workgroups
   // that hold such rows run their own copy of the tile loop.
   constexpr int kPreciseKeys = 256;
-  const bool precise_wg = ctx + tok0 < kPreciseKeys;  // group-uniform
+  const bool precise_wg = CROSS ? kv_end <= kPreciseKeys : ctx + tok0 < kPreciseKeys;  // group-uniform
   // The scaled-Q form (measurement switch): 2.5 instead of 3.5 VALU instructions per score.  At
   // head_dim 64, where halving the MFMAs per score leaves the softmax phase longer than the other
   // wave's matrix phase, it was 9 % faster on whole tiles (prefill_solo.h's now); at head_dim 128 it changes nothing.  It is not the
@@ -658,7 +669,7 @@ __global__ __launch_bounds__(512, 2) void prefill_kernel(Args a) {
     }
   }
   const int wtok_first = tok0 + ((wc * 32) >> a.gshift);
-  const int wlim_min = min(ctx + wtok_first + 1, kv_end);  // keys that all of the wave's columns see
+  const int wlim_min = CROSS ? kv_end : min(ctx + wtok_first + 1, kv_end);  // keys that all of the wave's columns see
 
   f32x16 o[G::kDBlocks];
 #pragma unroll

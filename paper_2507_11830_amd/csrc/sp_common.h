@@ -42,6 +42,30 @@ int launch_chunk_step(const sp_cache_desc &c, const void *k_new, const void *v_n
 size_t prefill_workspace_bytes(int batch, int total_q_tokens, int max_q_len, int max_kv_len, int num_q_heads,
                                int num_kv_heads, int head_dim);
 
+// Attention without a mask (sp_attn_cross); launchers as for the prefill.
+int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens,
+                 const int32_t *block_table, int batch, int max_pages, int total_q, int max_q_len, int max_kv_len,
+                 int num_q_heads, float scale, void *workspace, size_t workspace_bytes, hipStream_t stream);
+size_t cross_workspace_bytes(int batch, int total_q, int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim);
+
+// Norms, rotation and append in one pass; strides in elements.  k NULL: queries only.
+int launch_norm_rope_append(const sp_cache_desc &c, const void *q, const void *k, const void *v, long q_stride, long k_stride,
+                            long v_stride, void *q_out, const void *q_weight, const void *k_weight, float eps, const sp_rope_desc *rope,
+                            const int32_t *positions, const int32_t *cu_new, const int32_t *ctx_lens, const int32_t *block_table,
+                            int batch, int max_pages, int total_new, int num_q_heads, hipStream_t stream);
+
+// Pages (pages.hip).
+size_t pages_workspace_bytes(int num_pages, int n);
+int launch_pages_reserve(const sp_page_table &t, const int32_t *rows, const int32_t *new_lens, int n, int32_t *shortfall, void *workspace,
+                         hipStream_t stream);
+int launch_pages_fork(const sp_page_table &t, const int32_t *parents, const int32_t *children, int n, int32_t *copy_src, int32_t *copy_dst,
+                      int32_t *copy_rows, int32_t *shortfall, void *workspace, hipStream_t stream);
+int launch_pages_release(const sp_page_table &t, const int32_t *rows, const int32_t *keep_lens, int n, hipStream_t stream);
+int launch_pages_compact(const sp_page_table &t, int32_t *new_block_table, int32_t *new_ref_counts, int32_t *move_src, int32_t *move_dst,
+                         int32_t *moved, void *workspace, hipStream_t stream);
+int launch_pages_copy(const sp_cache_desc *caches, int num_caches, const int32_t *src, const int32_t *dst, const int32_t *rows,
+                      const int32_t *count, int n, hipStream_t stream);
+
 // [T_loc][H][d] <-> [P][T_loc][H/P][d] (pack = to the blocked side), bf16 elements.
 int launch_ulysses(bool pack, const void *src, void *dst, int T_loc, int H, int d, int P, hipStream_t stream);
 

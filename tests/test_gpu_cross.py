@@ -1,0 +1,230 @@
+"""sp_attn_cross against its definition in 64 bits: lengths on both sides, head layouts, the kernels behind it, empty encoders,
+workspaces, sub-ranges, graphs."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2507_11830_amd as sp
+from harness import kernel_launches
+
+pytestmark = pytest.mark.gpu
+
+
+class Case:
+    def __init__(self, heads, nq, nk, seed=0, scale=None, spread=1.0, poison=True):
+        self.hq, self.hkv, self.d = heads
+        self.nq, self.nk = np.array(nq), np.array(nk)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        need = [-(-int(n) // 16) for n in nk]
+        self.num_pages = max(1, sum(need) + 2)
+        perm = torch.randperm(self.num_pages, generator=torch.Generator().manual_seed(seed)).numpy().astype(np.int32)
+        table = np.full((len(nk), max(1, max(need))), -1, np.int32)
+        at = 0
+        for s, n in enumerate(need):
+            table[s, :n] = perm[at:at + n]
+            at += n
+        shape = (self.num_pages, self.hkv, 16, self.d)
+        k, v = (torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+        self.table = torch.from_numpy(table).cuda()
+        if poison:  # what lies behind a sequence's last key, and in pages that nobody holds
+            there = torch.zeros(self.num_pages, 16, dtype=torch.bool)
+            for s, n in enumerate(nk):
+                pos = np.arange(n)
+                there[table[s, pos // 16], pos % 16] = True
+            for p in (k, v):
+                p.masked_fill_(~there.cuda()[:, None, :, None], float("nan"))
+        self.cache = sp.KVCache(k, v)
+        self.T = int(sum(nq))
+        self.q = (torch.randn((self.T, self.hq, self.d), generator=g, device="cuda") * spread).to(torch.bfloat16)
+        self.out = torch.full_like(self.q, float("nan"))
+        self.cu = torch.tensor(np.concatenate([[0], np.cumsum(nq)]), dtype=torch.int32).cuda()
+        self.lens = torch.tensor(self.nk, dtype=torch.int32).cuda()
+        self.scale = 1 / math.sqrt(self.d) if scale is None else scale
+        self.max_q, self.max_kv = int(max(nq)), int(max(nk))
+
+    def workspace(self, short=0):
+        n = sp.sp_attn_cross_workspace_size(len(self.nq), self.T, self.max_q, self.max_kv, self.hq, self.hkv, self.d)
+        return torch.empty(max(n - short, 0), dtype=torch.uint8, device="cuda") if n else None
+
+    def call(self, ws):
+        sp.sp_attn_cross(self.cache, self.q, self.out, self.cu, self.lens, self.table, self.max_q, self.max_kv, self.scale, workspace=ws)
+
+    def definition(self, s):
+        """(out, sum of weights times |v|) of sequence s in 64 bits."""
+        a, b = int(self.cu[s]), int(self.cu[s + 1])
+        n, grp = int(self.nk[s]), self.hq // self.hkv
+        q = self.q[a:b].double().view(b - a, self.hkv, grp, self.d).permute(1, 2, 0, 3).reshape(self.hkv, -1, self.d)
+        pos = torch.arange(n, device="cuda")
+        page = self.table[s].long()[pos // 16]
+        k, v = (p[page, :, pos % 16].double().permute(1, 0, 2).contiguous() for p in (self.cache.k_pages, self.cache.v_pages))
+        w = torch.softmax(torch.bmm(q, k.transpose(1, 2).contiguous()) * self.scale, dim=-1)
+        back = lambda x: x.view(self.hkv, grp, b - a, self.d).permute(2, 0, 1, 3).reshape(b - a, self.hq, self.d)
+        return back(torch.bmm(w, v)), back(torch.bmm(w, v.abs()))
+
+    def check(self, seqs=None):
+        """Half a bf16 step of the output (2^-8), the same of every weight where a row has more than 256 keys (shorter rows take
+        their weights as hi + lo), and 2^-13 for fp32 sums of 128 products in the exponent of scores of order ten."""
+        got = self.out.double()
+        for s in range(len(self.nq)) if seqs is None else seqs:
+            a, b = int(self.cu[s]), int(self.cu[s + 1])
+            if a == b:
+                continue
+            x = got[a:b]
+            if self.nk[s] == 0:
+                assert (x == 0).all(), s
+                continue
+            want, size = self.definition(s)
+            most = 2.0**-8 * want.abs() + (2.0**-13 + (2.0**-8 if self.nk[s] > 256 else 0)) * size
+            assert torch.isfinite(x).all(), s
+            assert ((x - want).abs() <= most).all(), (s, float(((x - want).abs() - most).max()))
+
+
+SHARDS = [(2, 1, 64), (8, 1, 128), (32, 8, 128), (12, 3, 64), (16, 2, 64), (5, 5, 128), (12, 2, 128), (64, 1, 128), (7, 1, 64)]
+
+
+@pytest.mark.parametrize("heads", SHARDS, ids=str)
+@pytest.mark.parametrize("nq,nk", [
+    ([1, 1, 1, 1], [1, 37, 0, 500]),
+    ([3, 0, 4, 1, 2], [16, 90, 64, 0, 700]),
+    ([1, 70, 33, 0, 128, 257], [129, 15, 0, 4, 64, 65]),
+    ([300, 40], [1, 1000]),
+    ([2, 600, 31], [257, 256, 300]),
+], ids=("tokens", "few", "mixed", "long-q", "edges"))
+def test_lengths_and_heads(heads, nq, nk):
+    c = Case(heads, nq, nk, seed=len(nq))
+    for ws in (c.workspace(), None):
+        c.out.fill_(float("nan"))
+        c.call(ws)
+        c.check()
+
+
+@pytest.mark.parametrize("heads", [(8, 1, 128), (16, 2, 64), (32, 8, 128)], ids=str)
+@pytest.mark.parametrize("n", (63, 64, 65, 127, 128, 129, 255, 256, 257))
+def test_tile_edges(heads, n):
+    c = Case(heads, [n, 40, 1], [n, n + 1, n - 1], seed=n)
+    c.call(c.workspace())
+    c.check()
+
+
+@pytest.mark.parametrize("heads,nq,nk", [
+    ((8, 1, 128), [1] * 64, None),  # equal shares or fixed splits of the decode kernel
+    ((8, 1, 128), [1] * 200, None),
+    ((16, 2, 64), [4] * 40, None),
+    ((4, 1, 128), [16] * 6, None),  # two column tiles
+    ((4, 4, 64), [50, 3, 64], [3000, 20, 0]),
+    ((8, 1, 128), [1], [30000]),
+    ((32, 8, 128), [2, 1], [9000, 5]),
+    ((8, 1, 128), [40, 70], [9000, 6000]),  # pieces of the key ranges
+    ((16, 2, 64), [100], [12000]),
+    ((8, 1, 128), [1000] * 6, [700, 0, 900, 400, 1500, 64]),  # whole tiles
+    ((16, 2, 64), [900] * 8, None),  # several workgroups a CU
+    ((32, 8, 128), [700, 1200, 30], [333, 2000, 100]),
+    ((2, 2, 64), [3000], [3001]),
+    ((12, 3, 64), [1] * 600, None),  # more sequences than shares are dealt for
+], ids=lambda x: "x".join(map(str, x[:3])) if x else "any")
+def test_kernels_behind_it(heads, nq, nk):
+    rng = np.random.default_rng(len(nq))
+    nk = list(rng.integers(1, 2500, len(nq))) if nk is None else nk
+    if len(nq) > 30:
+        nk[3] = nk[17] = 0
+    c = Case(heads, nq, nk, seed=5)
+    c.call(c.workspace())
+    pick = None if len(nq) < 30 else list(rng.choice(len(nq), 20, replace=False)) + [3, 17]
+    c.check(pick)
+    first = c.out.clone()
+    c.out.fill_(float("nan"))
+    c.call(c.workspace())
+    assert torch.equal(first.view(torch.int16), c.out.view(torch.int16))  # the same bits again
+
+
+def test_the_division_of_the_keys_is_taken():
+    """Few query tokens on long ranges: pieces and their merge; and with less workspace than asked for, fewer or none."""
+    c = Case((8, 1, 128), [40], [9000], seed=1)
+    ws = c.workspace()
+    c.call(ws)
+    grids = kernel_launches(lambda: c.call(ws))
+    assert len(grids) == 2 and grids[0][0][2] >= 4
+    for short in (1, ws.numel() // 2, ws.numel() - 5):
+        c.out.fill_(float("nan"))
+        c.call(c.workspace(short))
+        c.check()
+
+
+def test_equals_decode_where_both_apply():
+    c = Case((8, 1, 128), [1] * 30, list(range(1, 3001, 100)), seed=2)
+    c.call(c.workspace())
+    other = torch.empty_like(c.out)
+    ws = torch.empty(sp.sp_attn_decode_workspace_size(30, c.max_kv, 8, 128), dtype=torch.uint8, device="cuda")
+    sp.sp_attn_decode(c.cache, c.q, other, c.lens, c.table, c.max_kv, c.scale, ws)
+    c.check()
+    c.out = other
+    c.check()
+
+
+def test_large_scores_and_equal_keys():
+    c = Case((8, 1, 128), [130, 5], [700, 90], seed=3, spread=16.0)  # nearly one-hot rows
+    c.call(c.workspace())
+    c.check()
+    c.cache.k_pages.copy_(torch.where(torch.isnan(c.cache.k_pages), c.cache.k_pages, torch.zeros((), dtype=torch.bfloat16, device="cuda")))
+    c.call(c.workspace())  # all weights equal: the mean of the values
+    c.check()
+
+
+def test_lengths_beyond_the_table_row_are_cut_there():
+    c = Case((8, 1, 128), [20, 3, 200], [64, 32, 64], seed=4)
+    c.lens += 1000
+    c.nk = np.array([64, 64, 64])
+    c.table[1, 2:] = c.table[0, 2:]
+    c.cache.k_pages.nan_to_num_(0.0)
+    c.cache.v_pages.nan_to_num_(0.0)
+    c.max_kv = 64
+    for ws in (c.workspace(), None):
+        c.call(ws)
+        c.check()
+
+
+def test_no_states_at_all():
+    for nq in ([3, 1], [500, 2]):
+        c = Case((8, 2, 64), nq, [0, 0], seed=6)
+        c.call(c.workspace())
+        assert (c.out == 0).all()
+        c.out.fill_(float("nan"))
+        empty = torch.empty(2, 0, dtype=torch.int32, device="cuda")
+        c.lens.fill_(-3)
+        sp.sp_attn_cross(c.cache, c.q, c.out, c.cu, c.lens, empty, c.max_q, 0, c.scale)
+        assert (c.out == 0).all()
+
+
+def test_sub_ranges_and_padded_buffers():
+    c = Case((8, 1, 128), [5, 300, 2, 64], [100, 900, 0, 400], seed=7)
+    sp.sp_attn_cross(c.cache, c.q, c.out, c.cu[1:4], c.lens[1:3], c.table[1:3], 300, 900, c.scale, workspace=c.workspace())
+    c.check([1, 2])
+    assert torch.isnan(c.out[:5]).all() and torch.isnan(c.out[307:]).all()
+    few = Case((8, 1, 128), [4, 3, 1, 2], [100, 900, 0, 400], seed=8)
+    sp.sp_attn_cross(few.cache, few.q, few.out, few.cu[1:4], few.lens[1:3], few.table[1:3], 4, 900, few.scale, workspace=few.workspace())
+    few.check([1, 2])
+    assert torch.isnan(few.out[:4]).all() and torch.isnan(few.out[8:]).all()
+
+
+@pytest.mark.parametrize("nq,nk", [([1] * 8, [900] * 8), ([70, 3], [5000, 200]), ([2000], [1500])], ids=("tokens", "pieces", "tiles"))
+def test_captured(nq, nk):
+    c = Case((8, 1, 128), nq, nk, seed=9)
+    ws = c.workspace()
+    c.call(ws)
+    g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(g, stream=side):
+            c.call(ws)
+    torch.cuda.current_stream().wait_stream(side)
+    for i in range(4):
+        c.q.normal_()
+        c.lens.sub_(7 * i)
+        c.call(ws)
+        want = c.out.clone()
+        c.out.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(want.view(torch.int16), c.out.view(torch.int16))
