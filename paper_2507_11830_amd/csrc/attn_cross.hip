@@ -8,19 +8,21 @@
 // keys are written as zeros.  Bound: bf16 MFMA, 4 * head_dim operations per (query, key) pair and head, for long chunks; HBM, the
 // states once for all query heads and tokens, for chunks of a few tokens.
 //
-// What is chosen from the hints, by the same measured rules as in attn_prefill.hip where the question is the same:
-//   - chunks of a few tokens (one or two column tiles of a wave): the decode kernel with equal shares or fixed splits;
-//   - otherwise query tiles of 256 columns (128 at head_dim 64, several workgroups a CU); on grids that do not fill the chip, of 128
-//     columns whose two wave groups take alternate key tiles, and where even these leave most CUs idle and the key ranges
-//     are long, in pieces of the key range.
+// What is chosen from the hints (cross_plan.h says when, and what it measured):
+//   - chunks of a few tokens, one column tile of a wave: the decode kernel with equal shares or fixed splits (75 batches of
+//     1 to 200 such chunks on 20 to 8000 keys: 22 % faster than query tiles in the mean).  With two column tiles, as in the causal calls,
+//     it took 13 % longer than query tiles in pieces (75 batches);
+//   - otherwise query tiles of 256 columns (128 at head_dim 64, several workgroups a CU), or of 128 columns whose two wave groups take
+//     alternate key tiles, and where even these leave most CUs idle, in pieces of the key range.
 #include "decode_stream.h"
 #include "prefill_solo.h"
+#include "cross_plan.h"
 
 namespace sp {
 
 // ---- chunks of a few tokens
-template <int D, int NT>
-__global__ __launch_bounds__(64 * kWaves, NT > 1 ? 1 : 2) void cross_stream_kernel(DecodeArgs a) {
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void cross_stream_kernel(DecodeArgs a) {
   extern __shared__ __align__(16) char smem_raw[];
   lds_char *smem = (lds_char *)smem_raw;
   const int lane = threadIdx.x & 63;
@@ -37,18 +39,18 @@ __global__ __launch_bounds__(64 * kWaves, NT > 1 ? 1 : 2) void cross_stream_kern
       else if ((int)threadIdx.x < a.cols) *reinterpret_cast<f32x2 *>(a.part_ml + 2 * ((long)slot * a.cols + threadIdx.x)) = (f32x2){-INFINITY, 0.f};
       return;
     }
-    row_segment<D, false, true, NT, true>(a, smem, lane, w, seq, hg, L, L - qn, tok, p0, p1, pages, a.row_splits == 1, slot);
+    row_segment<D, false, true, 1, true>(a, smem, lane, w, seq, hg, L, L - qn, tok, p0, p1, pages, a.row_splits == 1, slot);
     return;
   }
-  decode_share<D, false, true, NT, true>(a, smem, lane, w, blockIdx.x);
+  decode_share<D, false, true, 1, true>(a, smem, lane, w, blockIdx.x);
 }
 
-template <int D, int NT>
+template <int D>
 static int launch_cross_stream(const DecodeArgs &a, dim3 wgs, int max_pieces, hipStream_t stream) {
   static bool done = false;
   constexpr int smem = kDecodeShareSmem<D, true>;
-  if (int rc = grant_smem((const void *)cross_stream_kernel<D, NT>, &done, smem)) return rc;
-  hipLaunchKernelGGL((cross_stream_kernel<D, NT>), wgs, dim3(64 * kWaves), smem, stream, a);
+  if (int rc = grant_smem((const void *)cross_stream_kernel<D>, &done, smem)) return rc;
+  hipLaunchKernelGGL((cross_stream_kernel<D>), wgs, dim3(64 * kWaves), smem, stream, a);
   if (a.row_splits != 1) launch_decode_combine(a, max_pieces, D, stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SP_OK : fail(SP_ERR_HIP, "sp_attn_cross launch: %s", hipGetErrorString(e));
@@ -72,33 +74,39 @@ static int column_shift(int group) {  // log2 of the heads that share the column
   return gshift;
 }
 
-// Pieces of the key ranges of a launch of long chunks.
-static int cross_pieces(long rows, long wg128, int max_kv_len) {
-  if (!is_small_grid(wg128)) return 1;
-  const int kvs = kv_pieces(wg128, max_kv_len), cap = kv_split_cap(rows);
-  return kvs < 1 ? 1 : kvs < cap ? kvs : cap;
+// The calling thread's launch overrides (sp_debug_set_tuning) in the place of what cross_shape chooses.
+static CrossShape shape_of(int batch, int total_q, int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim, bool can_cut) {
+  const PrefillTuning tune = prefill_tuning();
+  const long rows = (long)total_q * num_q_heads;
+  const int gshift = column_shift(num_q_heads / num_kv_heads);
+  CrossShape s = cross_shape(rows, batch, (long)batch * (num_q_heads >> gshift), 1 << gshift, total_q, max_q_len, max_kv_len, head_dim,
+                             can_cut && tune.split == 0);
+  if (tune.kv_splits > 0 && can_cut) s.pieces = tune.kv_splits < kv_split_cap(rows) ? tune.kv_splits : kv_split_cap(rows);
+  if (tune.split > 0) s.halves = tune.split == 2;
+  if (tune.order > 0) s.ranked = tune.order == 2;
+  s.ranked = s.ranked && batch <= 64 * kRankSlots;
+  return s;
 }
 
 size_t cross_workspace_bytes(int batch, int total_q, int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim) {
   const long rows = (long)total_q * num_q_heads;
-  const int n_hgroups = num_q_heads >> column_shift(num_q_heads / num_kv_heads);
-  const int kvs = cross_pieces(rows, estimate_wg128(rows, batch, n_hgroups), max_kv_len);
+  const int kvs = shape_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim, true).pieces;
   const size_t pieces = kvs > 1 ? (size_t)rows * kvs * (head_dim + 2) * sizeof(float) : 0;
-  const size_t few = decode_multi_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim);
+  const size_t few = prefill_tuning().short_chunk == 1 || max_q_len > decode_route_cap(num_q_heads, num_kv_heads) ? 0 : decode_multi_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim);
   return pieces > few ? pieces : few;
 }
 
 int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens, const int32_t *block_table,
                  int batch, int max_pages, int total_q, int max_q_len, int max_kv_len, int num_q_heads, float scale, void *workspace,
                  size_t workspace_bytes, hipStream_t stream) {
-  {
+  const PrefillTuning tune = prefill_tuning();
+  if (tune.short_chunk != 1) {
     DecodeArgs d;
     dim3 wgs;
     int pieces = 0;
-    const int tiles = plan_decode_cross(d, c, q, out, cu_q, kv_lens, block_table, batch, max_pages, max_q_len, max_kv_len, num_q_heads, scale,
-                                        workspace, workspace_bytes, &wgs, &pieces);
-    if (tiles == 1) return c.head_dim == 128 ? launch_cross_stream<128, 1>(d, wgs, pieces, stream) : launch_cross_stream<64, 1>(d, wgs, pieces, stream);
-    if (tiles == 2) return c.head_dim == 128 ? launch_cross_stream<128, 2>(d, wgs, pieces, stream) : launch_cross_stream<64, 2>(d, wgs, pieces, stream);
+    if (plan_decode_cross(d, c, q, out, cu_q, kv_lens, block_table, batch, max_pages, max_q_len, max_kv_len, num_q_heads, scale, workspace, workspace_bytes,
+                          &wgs, &pieces))
+      return c.head_dim == 128 ? launch_cross_stream<128>(d, wgs, pieces, stream) : launch_cross_stream<64>(d, wgs, pieces, stream);
   }
   CrossArgs a = {};
   a.k_pages = (const char *)c.k_pages;
@@ -118,18 +126,21 @@ int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t
   a.tau = 8.0f / a.sl2e;
   a.batch = batch;
   a.total_q = total_q;
-  const long rows = (long)total_q * num_q_heads, streams = (long)batch * a.n_hgroups, wg128 = estimate_wg128(rows, batch, a.n_hgroups);
-  int kvs = workspace ? cross_pieces(rows, wg128, max_kv_len) : 1;
+  const long rows = (long)total_q * num_q_heads;
+  CrossShape shape = shape_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, c.num_kv_heads, c.head_dim, workspace != nullptr);
+  int kvs = shape.pieces;
   const size_t fit = workspace_bytes / ((size_t)rows * (c.head_dim + 2) * sizeof(float));
-  if ((size_t)kvs > fit) kvs = fit > 1 ? (int)fit : 1;
+  if ((size_t)kvs > fit) {  // fewer pieces, or the shape without any
+    kvs = fit > 1 ? (int)fit : 1;
+    if (kvs == 1) shape = shape_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, c.num_kv_heads, c.head_dim, false);
+  }
   a.kv_splits = kvs;
   a.part_o = (float *)workspace;
   a.part_ml = a.part_o + (size_t)rows * kvs * c.head_dim;
-  // Key ranges of different lengths: longest first.
-  a.ranked = batch >= 2 && batch <= 64 * kRankSlots;
+  a.ranked = shape.ranked;
   a.rank_shift = 6;
   while (a.rank_shift < 24 && (((long)max_kv_len + max_q_len) >> a.rank_shift) > 63) ++a.rank_shift;
-  const bool split = kvs > 1 || (is_small_grid(wg128) && !whole_tiles_pay(rows, streams, max_kv_len));
+  const bool split = kvs > 1 || shape.halves;
   const int rc = c.head_dim == 128 ? launch_cross_d<128>(a, split, batch, max_q_len, stream) : launch_cross_d<64>(a, split, batch, max_q_len, stream);
   if (rc != SP_OK || kvs == 1) return rc;
   return launch_combine(a.part_o, a.part_ml, out, rows, kvs, c.head_dim, stream, cu_q, batch, num_q_heads);

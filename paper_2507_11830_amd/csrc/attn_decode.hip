@@ -797,15 +797,14 @@ size_t decode_multi_workspace_bytes(int batch, int total_q, int max_q_len, int m
   return (size_t)total_q * num_q_heads * nsplit * (head_dim + 2) * sizeof(float);
 }
 
-int plan_decode_cross(DecodeArgs &a, const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens,
+bool plan_decode_cross(DecodeArgs &a, const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens,
                       const int32_t *block_table, int batch, int max_pages, int max_q_len, int max_kv_len, int num_q_heads, float scale,
                       void *workspace, size_t workspace_bytes, dim3 *grid, int *pieces) {
-  const int tiles = multi_shape(batch, max_q_len, num_q_heads, c.num_kv_heads, &a);
-  if (tiles == 0 || max_kv_len <= 0 || max_pages <= 0) return 0;
+  if (multi_shape(batch, max_q_len, num_q_heads, c.num_kv_heads, &a) != 1 || max_kv_len <= 0 || max_pages <= 0) return false;
   a.route_cap = 0;
   set_chunk_args(a, c, nullptr, nullptr, q, cu_q, kv_lens, block_table, max_pages, scale);
   a.out = (char *)out;
-  return plan_decode_stream(a, batch, max_q_len, tiles, max_kv_len, c.head_dim, workspace, workspace_bytes, 0, true, grid, pieces) ? 0 : tiles;
+  return plan_decode_stream(a, batch, max_q_len, 1, max_kv_len, c.head_dim, workspace, workspace_bytes, 0, true, grid, pieces) == 0;
 }
 
 // Mixed batches (sequences with a few query tokens next to sequences with long chunks, the usual

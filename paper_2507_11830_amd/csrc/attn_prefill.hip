@@ -38,6 +38,7 @@ void set_prefill_order(int mode) { g_order_mode = mode; }
 void set_prefill_short_chunk(int mode) { g_short_chunk_mode = mode; }
 void set_prefill_split(int mode) { g_split_mode = mode; }
 void set_prefill_kv_splits(int n) { g_kv_splits = n; }
+PrefillTuning prefill_tuning() { return {g_split_mode, g_kv_splits, g_short_chunk_mode, g_order_mode}; }
 
 // Mixed batch?  Decided from the host-side hints alone: chunks too long for the short-chunk path
 // exist (max_q_len), and the tokens besides the longest chunk are so few that at least one other

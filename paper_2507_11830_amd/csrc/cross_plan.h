@@ -1,0 +1,90 @@
+// How sp_attn_cross divides chunks of more than a few tokens over the chip, from the host-side hints alone.  Without a mask all query
+// tiles of a sequence are equally long, so the causal calls' rules (cut_plan.h), made for triangles, are not its own.  Plain code
+// that compiles for the host as well: the CPU tests run it.
+//
+// Times are estimated in us from constants that leave the least behind on 960 batches drawn at random (eight head shards, 1 to 24
+// sequences, up to 1600 workgroups of 128 columns, 20 to 8192 keys; equal lengths, unequal ones of both sides, unequal keys only;
+// all forms timed): 2.3 % over the best form of each batch, where the causal rules leave 7 %.  Both sides of it: 1 x 1137
+// queries on 4580 keys at 32q/4kv in halves 112 us (a second round of workgroups for the last tenth), whole tiles 88; 9 x 254 on 2133 at
+// 32q/8kv 98 and 107; 12 x 17..600 on 65..2500 at 12q/3kv, head_dim 64, 27 and 38.
+#pragma once
+#include "cut_plan.h"
+
+namespace sp {
+
+constexpr int kCus = 256;
+
+struct CrossShape {
+  bool halves;  // 128 columns, whose keys two wave groups share; else whole tiles of 256 (head_dim 64: 128, three workgroups a CU)
+  bool ranked;  // workgroups take the longest items first; else in (tile, sequence) order
+  int pieces;   // of the key ranges (halves only)
+};
+
+inline long ceil_div(long a, long b) { return (a + b - 1) / b; }
+
+// Pieces for launches that leave CUs idle: a key tile of a piece costs 0.4 us, the merge 2 us and 0.4 us per thousand partial rows of
+// 128 channels.
+// 4 x 14 queries on 2967 keys at 8q/1kv 31.6 us in one piece, 14.7 in 16; 1 x 168 on 1819 22.7, 19.1 in 4; 2 x 206 on 2284 at
+// 16q/2kv 27.7, 28.8 in 4.  All of them in one round of workgroups, with some room for the estimate.
+inline int cross_piece_count(long rows, long wgs, long max_kv_len, int head_dim) {
+  const long tiles = ceil_div(max_kv_len, 64);
+  const int cap = kv_split_cap(rows);
+  double least = 0.4 * tiles;
+  int best = 1;
+  for (int p = 2; p <= cap && p * wgs <= 240 && 2 * p <= tiles; ++p) {
+    const double t = 0.4 * ceil_div(tiles, p) + 2 + 0.4e-3 * rows * p * head_dim / 128;
+    if (t < least) {
+      least = t;
+      best = p;
+    }
+  }
+  return best;
+}
+
+// columns: query columns of a token (heads that share a KV head's column dimension); streams: sequences x head groups.
+inline CrossShape cross_shape(long rows, int batch, long streams, int columns, long total_q, long max_q_len, long max_kv_len, int head_dim,
+                              bool can_cut) {
+  const long tiles = ceil_div(max_kv_len, 64);
+  const long found = rows / 128 + (streams + 1) / 2, wgs = found > streams ? found : streams;  // workgroups of 128 columns that find work
+  const bool uneven = 10 * total_q < 9 * batch * max_q_len;
+  // The search for an item by its rank costs a microsecond per workgroup.  It pays where there is more than one round and the
+  // lengths differ: those of the queries are known; the keys' are taken to differ where they are not the queries' own, if the key
+  // ranges are long (8 x 270..1089 queries on 470..1891 keys at 16q/2kv, head_dim 64: 60 us by order, 45 ranked; 2 x 1904 on 101 at
+  // 32q/4kv 28.5 and 39.6).
+  auto rank = [&](int cols) { return batch >= 2 && streams * ceil_div(max_q_len * columns, cols) > kCus && (uneven ? tiles >= 2 : max_q_len != max_kv_len && tiles >= 30); };
+  CrossShape s;
+  s.pieces = can_cut ? cross_piece_count(rows, wgs, max_kv_len, head_dim) : 1;
+  const bool rank_halves = rank(128), rank_whole = rank(head_dim == 128 ? 256 : 128);
+  if (s.pieces > 1) {
+    s.halves = true;
+    s.ranked = rank_halves;
+    return s;
+  }
+  // A tile of an item: 0.55 us in halves, 1 whole; at head_dim 64 0.9, or 0.42 times the workgroups on its CU.  Starts, merges and
+  // stores: 10 us a round in halves, 9 whole.  Uneven batches: the mean item at 0.4 of the longest, and half of that (all of it by
+  // order) for the end.
+  const double n = (double)found;
+  auto span = [&](double items, double t, double start, bool ranked) {
+    if (!uneven) return (double)(long)((items + kCus - 1) / kCus) * (t + start);
+    const double even = items * (0.4 * t + start) / kCus + (ranked ? 0.5 : 1.0) * t;
+    return even > t + start ? even : t + start;
+  };
+  double whole;
+  if (head_dim == 128) {
+    whole = span(n / 2, 1.0 * tiles, 9, rank_whole);
+  } else if (uneven) {
+    const double even = n / kCus * 0.4 * 0.42 * tiles + 0.21 * tiles;
+    whole = 9 + (even > 0.9 * tiles ? even : 0.9 * tiles);
+  } else {
+    whole = 0;
+    for (long left = found; left > 0; left -= 3 * kCus) {
+      const long on_cu = left >= 3 * kCus ? 3 : ceil_div(left, kCus);
+      whole += (0.42 * on_cu > 0.9 ? 0.42 * on_cu : 0.9) * tiles + 9;
+    }
+  }
+  s.halves = span(n, 0.55 * tiles, 10, rank_halves) <= whole;
+  s.ranked = s.halves ? rank_halves : rank_whole;
+  return s;
+}
+
+}  // namespace sp

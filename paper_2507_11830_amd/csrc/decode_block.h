@@ -161,8 +161,8 @@ int launch_decode_stream(DecodeArgs &a, int batch, int max_q, int tiles, int max
 // to prefill workgroups), and the merge of the partials of a plan with row_splits 0 over query chunks.
 int plan_decode_stream(DecodeArgs &a, int batch, int max_q, int tiles, int max_len, int head_dim, void *workspace,
                        size_t workspace_bytes, int form, bool alone, dim3 *grid, int *pieces);
-// The same for chunks that attend without a mask: all arguments; returns the column tiles per wave, 0 where it does not qualify.
-int plan_decode_cross(DecodeArgs &a, const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens,
+// The same for chunks of one column tile that attend without a mask, all arguments.  False where it does not qualify.
+bool plan_decode_cross(DecodeArgs &a, const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens,
                       const int32_t *block_table, int batch, int max_pages, int max_q_len, int max_kv_len, int num_q_heads, float scale,
                       void *workspace, size_t workspace_bytes, dim3 *grid, int *pieces);
 void launch_decode_combine(const DecodeArgs &a, int max_pieces, int head_dim, hipStream_t stream);

@@ -8,7 +8,7 @@
 //
 // Launches: reserve and fork two (scan and plan; apply), compact three (scan; ranks; apply), release and copy one.  All but
 // the copy are bound by their chains of memory round trips, the copy by HBM.
-#include "sp_common.h"
+#include "attn_tile.h"
 
 namespace sp {
 
@@ -16,11 +16,11 @@ constexpr int kPageThreads = 256, kPageWaves = kPageThreads / 64;
 constexpr int kSegment = 4096;              // pages per workgroup of the scan
 constexpr int kSegWords = kSegment / 64;    // 64: one per lane
 
-template <typename T>
-static __device__ __forceinline__ T lane_prefix(T x) {  // inclusive sum over the lanes
+static __device__ __forceinline__ int lane_prefix(int x) { return wave_scan_incl(x); }
+static __device__ __forceinline__ long lane_prefix(long x) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const T y = __shfl_up(x, d);
+    const long y = __shfl_up(x, d);
     if ((int)(threadIdx.x & 63) >= d) x += y;
   }
   return x;
@@ -80,12 +80,12 @@ __global__ __launch_bounds__(kPageThreads) void pages_scan_kernel(PagesArgs p) {
     const long base = (long)blockIdx.x * kSegment + w * (PER * 64) + lane;
     int refs[PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) refs[i] = base + 64 * i < p.num_pages ? p.refs[base + 64 * i] : 1;
+    for (int i = 0; i < PER; ++i) refs[i] = p.refs[min(base + 64 * i, p.num_pages - 1L)];  // no branch: each load would wait for the one before
     uint64_t mine = 0;
     int free_pages = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const uint64_t bits = __builtin_amdgcn_ballot_w64(refs[i] <= 0);
+      const uint64_t bits = __builtin_amdgcn_ballot_w64(refs[i] <= 0 && base + 64 * i < p.num_pages);
       free_pages += __builtin_popcountll(bits);
       if (lane == i) mine = bits;
     }
@@ -131,47 +131,50 @@ __global__ __launch_bounds__(kPageThreads) void pages_scan_kernel(PagesArgs p) {
   }
 }
 
-// The free pages number first .. first + m - 1 of the pool in ascending order: take(k, page) for the k-th of them, k from 0, by any
-// thread.  c0: seg_free[threadIdx.x], 0 behind the last; by the whole workgroup.
-template <typename Take>
-static __device__ __forceinline__ void for_free_pages(const PagesArgs &p, int c0, int first, int m, int *wave_sums, int *seg_before, Take take) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int before = 0;
-  for (int s0 = 0; s0 < p.nseg && before < first + m; s0 += kPageThreads) {
-    const int s = s0 + threadIdx.x, c = s0 == 0 ? c0 : s < p.nseg ? p.seg_free[s] : 0;
+// Which segments hold the pool's free pages number `first` and on.  seg_before[q]: free pages before segment s0 + q, for the
+// kPageThreads segments from s0 on.
+struct FreePages {
+  int *wave_sums, *seg_before;  // LDS: kPageWaves and kPageThreads + 1 ints
+  int s0, upto;                 // upto: free pages before segment s0 + kPageThreads
+
+  // Segments from s on, of which `before` free pages lie before; by the whole workgroup.  c: seg_free of segment s + threadIdx.x, 0 behind the last.
+  __device__ __forceinline__ void look(int s, int before, int c) {
     int total;
-    const int incl = block_prefix(c, wave_sums, &total);
+    const int incl = block_prefix(c, wave_sums, &total);  // nobody reads seg_before any more when its barriers are passed
     seg_before[threadIdx.x + 1] = before + incl;
     if (threadIdx.x == 0) seg_before[0] = before;
     __syncthreads();
-    if (before + total > first) {
-      // the segments that hold such pages: from the first that ends behind `first` on
-      int lo = 0, hi = kPageThreads;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (seg_before[mid + 1] > first) hi = mid;
-        else lo = mid + 1;
-      }
-      for (int q = lo + w; q < kPageThreads && s0 + q < p.nseg && seg_before[q] < first + m; q += kPageWaves) {
-        uint64_t bits = p.free_bits[(long)(s0 + q) * kSegWords + lane];
-        const int mine = __builtin_popcountll(bits);
-        int k = seg_before[q] + lane_prefix(mine) - mine - first;
-        const int page = (s0 + q) * kSegment + 64 * lane;
-        for (; bits != 0 && k < m; bits &= bits - 1, ++k)
-          if (k >= 0) take(k, page + __builtin_ctzll(bits));
-      }
-    }
-    before += total;
+    s0 = s;
+    upto = before + total;
   }
-}
-
-// Free pages of the pool; c0 as above.
-static __device__ __forceinline__ int all_free(const PagesArgs &p, int c0, int *wave_sums) {
-  int c = c0, total;
-  for (int s = threadIdx.x + kPageThreads; s < p.nseg; s += kPageThreads) c += p.seg_free[s];
-  block_prefix(c, wave_sums, &total);
-  return total;
-}
+  // take(k, page) for k = 0 .. m - 1: the page that is number first + k of the free ones; by the whole workgroup, any thread takes any.
+  template <typename Take>
+  __device__ __forceinline__ void take_pages(const PagesArgs &p, int first, int m, Take take) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (;;) {
+      if (upto > first) {
+        int lo = 0, hi = kPageThreads;  // the first of these segments that ends behind `first`
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (seg_before[mid + 1] > first) hi = mid;
+          else lo = mid + 1;
+        }
+        for (int q = lo + w; q < kPageThreads && s0 + q < p.nseg && seg_before[q] < first + m; q += kPageWaves) {
+          uint64_t bits = p.free_bits[(long)(s0 + q) * kSegWords + lane];
+          const int mine = __builtin_popcountll(bits);
+          int k = seg_before[q] + lane_prefix(mine) - mine - first;
+          const int page = (s0 + q) * kSegment + 64 * lane;
+          for (; bits != 0 && k < m; bits &= bits - 1, ++k)
+            if (k >= 0) take(k, page + __builtin_ctzll(bits));
+        }
+      }
+      const int next = s0 + kPageThreads;
+      if (upto >= first + m || next >= p.nseg) return;  // uniform
+      const int s = next + threadIdx.x;
+      look(next, upto, s < p.nseg ? p.seg_free[s] : 0);
+    }
+  }
+};
 
 // One workgroup per entry.
 template <int OP>
@@ -179,8 +182,16 @@ __global__ __launch_bounds__(kPageThreads) void pages_take_kernel(PagesArgs p) {
   __shared__ int wave_sums[kPageWaves], seg_before[kPageThreads + 1], s_old, s_page;
   const int i = blockIdx.x, a = p.a[i], b = p.b[i];
   const int first = p.plan[i], need = p.plan[i + 1] - first, wanted = p.plan[p.n], size = p.sizes[i];
-  const int c0 = (int)threadIdx.x < p.nseg ? p.seg_free[threadIdx.x] : 0;
-  const int missing = max(wanted - all_free(p, c0, wave_sums), 0);
+  FreePages pool = {wave_sums, seg_before, 0, 0};
+  pool.look(0, 0, (int)threadIdx.x < p.nseg ? p.seg_free[threadIdx.x] : 0);
+  int all_free = pool.upto;
+  if (p.nseg > kPageThreads) {
+    int c = 0, more;
+    for (int s = threadIdx.x + kPageThreads; s < p.nseg; s += kPageThreads) c += p.seg_free[s];
+    block_prefix(c, wave_sums, &more);
+    all_free += more;
+  }
+  const int missing = max(wanted - all_free, 0);
   if (i == 0 && threadIdx.x == 0) *p.shortfall = missing;
   if constexpr (OP == kReserve) {
     if (missing > 0 || size == 0) return;  // size > 0: a is a row of the table, and holds no more pages than b takes
@@ -190,39 +201,39 @@ __global__ __launch_bounds__(kPageThreads) void pages_take_kernel(PagesArgs p) {
     const int has = pages_of(s_old), m = min(size - has, need);
     if (m <= 0) return;
     int32_t *row = p.table + (long)a * p.max_pages + has;
-    for_free_pages(p, c0, first, m, wave_sums, seg_before, [&](int k, int page) __attribute__((always_inline)) {
+    pool.take_pages(p, first, m, [&](int k, int page) __attribute__((always_inline)) {
       row[k] = page;
       p.refs[page] = 1;
     });
   } else {
     bool taken = missing == 0 && size >= 0;
-    if (taken && size > 0) {
-      if (threadIdx.x == 0) s_old = atomicCAS(p.lens + b, 0, size);
-      __syncthreads();
-      taken = s_old == 0;
-    }
-    if (threadIdx.x == 0 && !(taken && need > 0)) {
-      p.copy_src[i] = p.copy_dst[i] = -1;
-      p.copy_rows[i] = 0;
-    }
-    if (!taken) return;
+    const int full = taken ? size / kPage : 0;
     const int32_t *from = p.table + (long)a * p.max_pages;
     int32_t *to = p.table + (long)b * p.max_pages;
-    const int full = size / kPage;
+    // the parent's first pages, the new page and the claim of the child in one round trip
+    const int page0 = (int)threadIdx.x < full ? from[threadIdx.x] : -1;
+    int old = 0;
+    if (threadIdx.x == 0 && taken && size > 0) old = atomicCAS(p.lens + b, 0, size);
+    const int last = threadIdx.x == 0 && taken && need > 0 ? from[full] : -1;
+    if (taken && need > 0) pool.take_pages(p, first, 1, [&](int, int page) __attribute__((always_inline)) { s_page = page; });
+    if (threadIdx.x == 0) s_old = old;
+    __syncthreads();
+    taken = taken && s_old == 0;
+    if (threadIdx.x == 0) {
+      const bool copy = taken && need > 0;
+      if (copy) {
+        to[full] = s_page;
+        p.refs[s_page] = 1;
+      }
+      p.copy_src[i] = copy ? last : -1;
+      p.copy_dst[i] = copy ? s_page : -1;
+      p.copy_rows[i] = copy ? size % kPage : 0;
+    }
+    if (!taken) return;
     for (int c = threadIdx.x; c < full; c += kPageThreads) {
-      const int page = from[c];
+      const int page = c < kPageThreads ? page0 : from[c];
       to[c] = page;
       if (page >= 0 && page < p.num_pages) atomicAdd(p.refs + page, 1);
-    }
-    if (need == 0) return;
-    for_free_pages(p, c0, first, 1, wave_sums, seg_before, [&](int, int page) __attribute__((always_inline)) { s_page = page; });
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      to[full] = s_page;
-      p.refs[s_page] = 1;
-      p.copy_src[i] = from[full];
-      p.copy_dst[i] = s_page;
-      p.copy_rows[i] = size % kPage;
     }
   }
 }
@@ -233,12 +244,14 @@ __global__ __launch_bounds__(kPageThreads) void pages_release_kernel(PagesArgs p
   __shared__ int s_old;
   const int row = p.a[blockIdx.x], keep = keep_lens ? max(keep_lens[blockIdx.x], 0) : 0;
   if (row < 0 || row >= p.num_rows) return;
+  int32_t *entries = p.table + (long)row * p.max_pages;
+  const int c0 = (int)min((long)pages_of(keep) + threadIdx.x, (long)p.max_pages);
+  const int page0 = c0 < p.max_pages ? entries[c0] : -1;  // in the same round trip as the claim
   if (threadIdx.x == 0) s_old = atomicMin(p.lens + row, keep);
   __syncthreads();
   const int end = min(pages_of(s_old), p.max_pages);
-  int32_t *entries = p.table + (long)row * p.max_pages;
-  for (int c = pages_of(keep) + threadIdx.x; c < end; c += kPageThreads) {
-    const int page = entries[c];
+  for (int c = c0; c < end; c += kPageThreads) {
+    const int page = c == c0 ? page0 : entries[c];
     entries[c] = -1;
     if (page >= 0 && page < p.num_pages) atomicSub(p.refs + page, 1);
   }

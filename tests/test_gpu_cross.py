@@ -112,7 +112,7 @@ def test_tile_edges(heads, n):
     ((8, 1, 128), [1] * 64, None),  # equal shares or fixed splits of the decode kernel
     ((8, 1, 128), [1] * 200, None),
     ((16, 2, 64), [4] * 40, None),
-    ((4, 1, 128), [16] * 6, None),  # two column tiles
+    ((4, 1, 128), [16] * 6, None),  # more heads than a column tile holds tokens of
     ((4, 4, 64), [50, 3, 64], [3000, 20, 0]),
     ((8, 1, 128), [1], [30000]),
     ((32, 8, 128), [2, 1], [9000, 5]),
