@@ -294,7 +294,8 @@ int sp_norm_rope_append(const sp_cache_desc *cache, const void *q, const void *k
  * ceil(seq_lens[s] / 16) entries; ref_counts[p] is the number of entries that hold page p; a page is free if that is 0.
  * Free pages are always taken in ascending order, for the entries of a call's list in their order: results do not
  * depend on timing.
- * Out-of-range rows and page ids are skipped; lengths count as at most max_pages_per_seq * 16.
+ * Out-of-range rows and page ids are skipped; lengths count as at most max_pages_per_seq * 16.  Calls on one table are
+ * ordered by the caller (one stream, or events between them).
  */
 typedef struct sp_page_table {
   int32_t *ref_counts;  /* device, int32 [num_pages]                                            */
@@ -320,8 +321,9 @@ int sp_pages_reserve(const sp_page_table *table, const int32_t *rows, const int3
  * is not full, a page of its own for it, whose rows the caller copies with sp_pages_copy in the cache of every layer:
  *   copy_src, copy_dst, copy_rows  int32 [n] (device, written): rows 0 .. copy_rows[i] - 1 of page copy_src[i] belong into
  *              page copy_dst[i]; -1, -1 and 0 where there is nothing to copy
- * A child is an empty row (seq_lens 0), and named once; entries whose child is not empty are skipped, and of several entries
- * for one child an unspecified one is taken.  All entries or none, shortfall and workspace: as in sp_pages_reserve.
+ * Lengths are those before the call: a parent that is empty then leaves its children empty.  A child is an empty row (seq_lens
+ * 0), and named once; entries whose child is not empty are skipped, and of several entries for one child an unspecified one
+ * is taken.  All entries or none, shortfall and workspace: as in sp_pages_reserve.
  */
 int sp_pages_fork(const sp_page_table *table, const int32_t *parents, const int32_t *children, int32_t n,
                   int32_t *copy_src, int32_t *copy_dst, int32_t *copy_rows, int32_t *shortfall,

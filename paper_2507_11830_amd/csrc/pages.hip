@@ -238,6 +238,105 @@ __global__ __launch_bounds__(kPageThreads) void pages_take_kernel(PagesArgs p) {
   }
 }
 
+// Few entries on a small pool: scan, plan and entries in one workgroup, a wave per entry, so one launch instead of two.  Of several
+// entries for one child the first is taken, and entries for one row get their room one after the other.
+constexpr int kSmallWaves = 16, kSmallPages = kSmallWaves * 1024, kSmallWidth = 1024;
+
+template <int OP>
+__global__ __launch_bounds__(64 * kSmallWaves) void pages_small_kernel(PagesArgs p) {
+  constexpr int PER = 16;                               // words of a wave
+  constexpr int WORDS = kSmallWaves * PER, LANE = WORDS / 64;
+  __shared__ uint64_t s_bits[WORDS];
+  __shared__ int s_a[kSmallWaves], s_b[kSmallWaves], s_size[kSmallWaves], s_first[kSmallWaves + 1];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int refs[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) refs[i] = p.refs[min(1024 * w + 64 * i + lane, p.num_pages - 1)];
+  if (w == 0) {
+    const bool mine = lane < p.n;
+    const int a = mine ? p.a[lane] : -1, b = mine ? p.b[lane] : -1;
+    const bool row = a >= 0 && a < p.num_rows, child = OP == kFork && row && b >= 0 && b < p.num_rows;
+    const int tokens = row ? row_tokens(p, a) : 0, child_len = child ? p.lens[b] : 1;
+    int size = OP == kFork ? (child && child_len == 0 ? tokens : -1) : (row && pages_of(b) <= p.max_pages ? pages_of(b) : 0);
+    int has = pages_of(tokens);
+    for (int j = 0; j < p.n - 1; ++j) {  // entries before this one
+      const int aj = __builtin_amdgcn_readlane(a, j), bj = __builtin_amdgcn_readlane(b, j), sj = __builtin_amdgcn_readlane(size, j);
+      if (j >= lane) continue;
+      if (OP == kFork && bj == b && sj > 0) size = -1;
+      if (OP == kReserve && aj == a) has = max(has, sj);
+    }
+    const int need = OP == kFork ? (size > 0 && size % kPage != 0) : max(size - has, 0);
+    const int incl = wave_scan_incl(need);  // entries of at most kSmallWidth pages: no overflow
+    if (mine) {
+      s_a[lane] = a;
+      s_b[lane] = b;
+      s_size[lane] = size;
+      s_first[lane] = incl - need;
+      if (lane == p.n - 1) s_first[p.n] = incl;
+    }
+  }
+  uint64_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint64_t bits = __builtin_amdgcn_ballot_w64(refs[i] <= 0 && 1024 * w + 64 * i + lane < p.num_pages);
+    if (lane == i) mine = bits;
+  }
+  if (lane < PER) s_bits[w * PER + lane] = mine;
+  __syncthreads();
+  if (w >= p.n) return;
+  // every wave by itself: its entry, and the free pages before each of the lane's words
+  uint64_t bits[LANE];
+  int count = 0;
+#pragma unroll
+  for (int i = 0; i < LANE; ++i) {
+    bits[i] = s_bits[LANE * lane + i];
+    count += __builtin_popcountll(bits[i]);
+  }
+  const int incl = wave_scan_incl(count), all_free = __builtin_amdgcn_readlane(incl, 63);
+  const int missing = max(s_first[p.n] - all_free, 0);
+  if (w == 0 && lane == 0) *p.shortfall = missing;
+  const int a = s_a[w], b = s_b[w], size = s_size[w], first = s_first[w], need = s_first[w + 1] - first;
+  auto take_pages = [&](auto take) __attribute__((always_inline)) {
+    int k = incl - count - first;
+#pragma unroll
+    for (int i = 0; i < LANE; ++i)
+      for (uint64_t left = bits[i]; left != 0 && k < need; left &= left - 1, ++k)
+        if (k >= 0) take(k, 64 * (LANE * lane + i) + __builtin_ctzll(left));
+  };
+  if constexpr (OP == kReserve) {
+    if (missing > 0 || size == 0) return;
+    if (lane == 0) atomicMax(p.lens + a, b);
+    int32_t *row = p.table + (long)a * p.max_pages + size - need;
+    take_pages([&](int k, int page) __attribute__((always_inline)) {
+      row[k] = page;
+      p.refs[page] = 1;
+    });
+  } else {
+    const bool taken = missing == 0 && size >= 0;
+    if (!(taken && need > 0) && lane == 0) {
+      p.copy_src[w] = p.copy_dst[w] = -1;
+      p.copy_rows[w] = 0;
+    }
+    if (!taken || size == 0) return;
+    const int32_t *from = p.table + (long)a * p.max_pages;
+    int32_t *to = p.table + (long)b * p.max_pages;
+    const int full = size / kPage;
+    if (lane == 0) p.lens[b] = size;
+    take_pages([&](int, int page) __attribute__((always_inline)) {
+      p.copy_src[w] = from[full];
+      p.copy_dst[w] = page;
+      p.copy_rows[w] = size % kPage;
+      to[full] = page;
+      p.refs[page] = 1;
+    });
+    for (int c = lane; c < full; c += 64) {
+      const int page = from[c];
+      to[c] = page;
+      if (page >= 0 && page < p.num_pages) atomicAdd(p.refs + page, 1);
+    }
+  }
+}
+
 // One workgroup per entry.  Lowering the length claims the pages behind it, so of several entries for one row each gives back
 // different ones.
 __global__ __launch_bounds__(kPageThreads) void pages_release_kernel(PagesArgs p, const int32_t *keep_lens) {
@@ -263,6 +362,10 @@ __global__ __launch_bounds__(kPageThreads) void pages_rank_kernel(PagesArgs p) {
   __shared__ int wave_sums[kPageWaves], s_before[kSegWords], s_seg[2];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, seg = blockIdx.x;
   const uint64_t my_bits = p.free_bits[(long)seg * kSegWords + lane];
+  constexpr int PER = kSegWords / kPageWaves;
+  int refs[PER];  // requested first: inside the loop below every count would be waited for by itself (a pool of 4138 pages 7.9 us)
+#pragma unroll
+  for (int i = 0; i < PER; ++i) refs[i] = p.refs[min((long)seg * kSegment + 64 * (w + i * kPageWaves) + lane, p.num_pages - 1L)];
   int sum = 0, below = 0, total_free, before_seg;
   for (int s = threadIdx.x; s < p.nseg; s += kPageThreads) {
     const int c = p.seg_free[s];
@@ -292,7 +395,9 @@ __global__ __launch_bounds__(kPageThreads) void pages_rank_kernel(PagesArgs p) {
     s_before[lane] = before_seg + lane_prefix(c) - c;
   }
   __syncthreads();
-  for (int k = w; k < kSegWords; k += kPageWaves) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int k = w + i * kPageWaves;
     const long page = (long)seg * kSegment + 64 * k + lane;
     const uint64_t bits = __shfl(my_bits, k);  // by all lanes
     if (page >= p.num_pages) continue;
@@ -305,7 +410,7 @@ __global__ __launch_bounds__(kPageThreads) void pages_rank_kernel(PagesArgs p) {
       const int r = (int)page - free_before - (used - holes);
       p.move_src[r] = (int)page;
       p.rank[page] = r;
-      p.moved_refs[r] = p.refs[page];
+      p.moved_refs[r] = refs[i];
     }
   }
 }
@@ -407,14 +512,24 @@ static int launched(const char *what) {
   return e == hipSuccess ? SP_OK : fail(SP_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
 }
 
+// Scan and take, or both in one launch: 4 forks of a row of 19 pages in a pool of 160 6.7 us (kernels alone) as two launches.
+template <int OP>
+static void launch_take(const PagesArgs &p, hipStream_t stream) {
+  if (p.n <= kSmallWaves && p.num_pages <= kSmallPages && p.max_pages <= kSmallWidth) {
+    hipLaunchKernelGGL(pages_small_kernel<OP>, dim3(1), dim3(64 * kSmallWaves), 0, stream, p);
+    return;
+  }
+  hipLaunchKernelGGL(pages_scan_kernel<OP>, dim3(p.nseg + 1), dim3(kPageThreads), 0, stream, p);
+  hipLaunchKernelGGL(pages_take_kernel<OP>, dim3(p.n), dim3(kPageThreads), 0, stream, p);
+}
+
 int launch_pages_reserve(const sp_page_table &t, const int32_t *rows, const int32_t *new_lens, int n, int32_t *shortfall, void *workspace,
                          hipStream_t stream) {
   PagesArgs p = pages_args(t, workspace, n);
   p.a = rows;
   p.b = new_lens;
   p.shortfall = shortfall;
-  hipLaunchKernelGGL(pages_scan_kernel<kReserve>, dim3(p.nseg + 1), dim3(kPageThreads), 0, stream, p);
-  hipLaunchKernelGGL(pages_take_kernel<kReserve>, dim3(n), dim3(kPageThreads), 0, stream, p);
+  launch_take<kReserve>(p, stream);
   return launched("sp_pages_reserve");
 }
 
@@ -427,8 +542,7 @@ int launch_pages_fork(const sp_page_table &t, const int32_t *parents, const int3
   p.copy_dst = copy_dst;
   p.copy_rows = copy_rows;
   p.shortfall = shortfall;
-  hipLaunchKernelGGL(pages_scan_kernel<kFork>, dim3(p.nseg + 1), dim3(kPageThreads), 0, stream, p);
-  hipLaunchKernelGGL(pages_take_kernel<kFork>, dim3(n), dim3(kPageThreads), 0, stream, p);
+  launch_take<kFork>(p, stream);
   return launched("sp_pages_fork");
 }
 

@@ -40,7 +40,7 @@ class Model:
         return 0
 
     def fork(self, parents, children):
-        rows = len(self.lens)
+        rows, before = len(self.lens), self.lens.copy()
         ok = [0 <= p < rows and 0 <= c < rows and self.lens[c] == 0 for p, c in zip(parents, children)]
         free, copies = self.free(), []
         need = sum(bool(o and self.lens[p] % 16) for o, p in zip(ok, parents))
@@ -50,7 +50,7 @@ class Model:
             copies.append((-1, -1, 0))
             if not o:
                 continue
-            n = self.lens[p]
+            n = before[p]
             for i in range(n // 16):
                 self.table[c, i] = self.table[p, i]
                 self.refs[self.table[p, i]] += 1
@@ -87,10 +87,11 @@ class Model:
 class Both:
     """A model and a device table that take the same calls."""
 
-    def __init__(self, rows, width, pages):
+    def __init__(self, rows, width, pages, pad=0):
+        self.pad = pad  # entries without a row behind every list: what longer lists take is another kernel
         self.m, self.t = Model(rows, width, pages), sp.PageTable.empty(rows, width, pages)
         self.short = dev([-7])
-        n = max(sp.sp_pages_workspace_size(pages, 4 * rows), sp.sp_pages_workspace_size(pages, 0))
+        n = max(sp.sp_pages_workspace_size(pages, 4 * rows + pad), sp.sp_pages_workspace_size(pages, 0))
         self.ws = torch.full((n,), 0xA5, dtype=torch.uint8, device="cuda")
 
     def same(self):
@@ -100,6 +101,7 @@ class Both:
         sp.sp_debug_validate_pages(self.t)
 
     def reserve(self, rows, new):
+        rows, new = [*rows, *[-1] * self.pad], [*new, *[5] * self.pad]
         want = self.m.reserve(rows, new)
         sp.sp_pages_reserve(self.t, dev(rows), dev(new), self.short, self.ws)
         assert int(self.short) == want
@@ -107,6 +109,7 @@ class Both:
         return want
 
     def fork(self, parents, children):
+        parents, children = [*parents, *[-1] * self.pad], [*children, *[0] * self.pad]
         want, copies = self.m.fork(parents, children)
         lists = [dev([-9] * len(parents)) for _ in range(3)]
         sp.sp_pages_fork(self.t, dev(parents), dev(children), *lists, self.short, self.ws)
@@ -134,11 +137,12 @@ class Both:
         return a, b, moved
 
 
-@pytest.mark.parametrize("pages", (1, 2, 63, 64, 65, 300, 4095, 4096, 4097, 9000))
-def test_random_lives(pages):
+@pytest.mark.parametrize("pad", (0, 30), ids=("short-lists", "long-lists"))
+@pytest.mark.parametrize("pages", (1, 2, 63, 64, 65, 300, 1023, 1025, 4095, 4096, 4097, 9000, 16383, 16384, 16385))
+def test_random_lives(pages, pad):
     rng = np.random.default_rng(pages)
     rows, width = 40, 30
-    b = Both(rows, width, pages)
+    b = Both(rows, width, pages, pad)
     for step in range(25):
         what = rng.choice(["reserve", "reserve", "fork", "release", "release", "keep", "compact"])
         pick = rng.choice(rows, rng.integers(1, 12), replace=False)
@@ -189,8 +193,9 @@ def test_a_pool_larger_than_one_round_of_segments():
     assert int(b.t.ref_counts[:used].min()) == 1 and int(b.t.ref_counts[used:].abs().max()) == 0
 
 
-def test_all_or_nothing():
-    b = Both(6, 8, 10)
+@pytest.mark.parametrize("pad", (0, 30))
+def test_all_or_nothing(pad):
+    b = Both(6, 8, 10, pad)
     b.reserve([0, 1], [100, 20])  # 7 + 2 pages: one is left
     assert b.reserve([2, 3], [16, 1]) == 1
     assert b.reserve([2, 3, 4], [128, 128, 128]) == 23
@@ -198,6 +203,25 @@ def test_all_or_nothing():
     b.fork([0], [4])
     b.release([4])
     b.reserve([5], [16])
+
+
+def test_lists_up_to_the_small_kernel_s_length():
+    for n in (1, 15, 16, 17):
+        b = Both(64, 40, 3000)
+        b.reserve(np.arange(n), 600 - 30 * np.arange(n))
+        b.fork(np.arange(n)[::-1], 20 + np.arange(n))
+        b.reserve(20 + np.arange(n), [640] * n)
+        b.fork([3, 40], [40, 41])  # the second parent is empty when the call is made
+        b.release(np.arange(64))
+
+
+def test_wide_tables():
+    for width in (1024, 1025):
+        b = Both(9, width, 9000)
+        b.reserve([0, 1, 2], [16 * width, 16 * width - 3, 5000])
+        b.fork([0, 1, 2], [5, 6, 7])
+        b.release([1, 5], [4000, 16 * width - 15])
+        b.compact(in_place=True)
 
 
 def test_lists_longer_than_a_workgroup():
@@ -209,21 +233,23 @@ def test_lists_longer_than_a_workgroup():
     b.compact(in_place=False)
 
 
-def test_skipped_entries():
-    b = Both(5, 4, 40)
+@pytest.mark.parametrize("pad", (0, 30))
+def test_skipped_entries(pad):
+    b = Both(5, 4, 40, pad)
     b.reserve([0, -1, 7, 1, 2], [33, 16, 16, 65, 64])  # rows outside the table, more than a row holds
     b.fork([0, 0, -3, 9, 1, 0], [2, 3, 4, 4, 4, -1])  # a child in use, rows outside, an empty parent
     b.release([-1, 5, 3], [1, 1, 1])
 
 
-def test_the_same_row_twice():
-    b = Both(4, 8, 64)
-    sp.sp_pages_reserve(b.t, dev([1, 1, 1]), dev([40, 100, 70]), b.short, b.ws)
+@pytest.mark.parametrize("pad", (0, 30))
+def test_the_same_row_twice(pad):
+    b, none = Both(4, 8, 64), [-1] * pad
+    sp.sp_pages_reserve(b.t, dev([1, 1, 1, *none]), dev([40, 100, 70, *none]), b.short, b.ws)
     sp.sp_debug_validate_pages(b.t)
     assert b.t.seq_lens.tolist() == [0, 100, 0, 0] and int(b.t.ref_counts.sum()) == 7
     sp.sp_pages_reserve(b.t, dev([0]), dev([25]), b.short, b.ws)
-    lists = [dev([0, 0]) for _ in range(3)]
-    sp.sp_pages_fork(b.t, dev([0, 1]), dev([2, 2]), *lists, b.short, b.ws)  # one of the two
+    lists = [dev([0, 0, *none]) for _ in range(3)]
+    sp.sp_pages_fork(b.t, dev([0, 1, *none]), dev([2, 2, *none]), *lists, b.short, b.ws)  # one of the two
     sp.sp_debug_validate_pages(b.t)
     assert int(b.t.seq_lens[2]) in (25, 100) and sum(x >= 0 for x in lists[0].tolist()) == 1
     sp.sp_pages_release(b.t, dev([1, 1, 1, 2, 2]), dev([50, 20, 90, 0, 0]))
