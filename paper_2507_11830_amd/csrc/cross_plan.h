@@ -46,12 +46,12 @@ inline CrossShape cross_shape(long rows, int batch, long streams, int columns, l
                               bool can_cut) {
   const long tiles = ceil_div(max_kv_len, 64);
   const long found = rows / 128 + (streams + 1) / 2, wgs = found > streams ? found : streams;  // workgroups of 128 columns that find work
-  const bool uneven = 10 * total_q < 9 * batch * max_q_len;
+  const bool uneven = 10.0 * total_q < 9.0 * batch * max_q_len;
   // The search for an item by its rank costs a microsecond per workgroup.  It pays where there is more than one round and the
   // lengths differ: those of the queries are known; the keys' are taken to differ where they are not the queries' own, if the key
   // ranges are long (8 x 270..1089 queries on 470..1891 keys at 16q/2kv, head_dim 64: 60 us by order, 45 ranked; 2 x 1904 on 101 at
   // 32q/4kv 28.5 and 39.6).
-  auto rank = [&](int cols) { return batch >= 2 && streams * ceil_div(max_q_len * columns, cols) > kCus && (uneven ? tiles >= 2 : max_q_len != max_kv_len && tiles >= 30); };
+  auto rank = [&](int cols) { return batch >= 2 && (double)streams * ceil_div(max_q_len * columns, cols) > kCus && (uneven ? tiles >= 2 : max_q_len != max_kv_len && tiles >= 30); };
   CrossShape s;
   s.pieces = can_cut ? cross_piece_count(rows, wgs, max_kv_len, head_dim) : 1;
   const bool rank_halves = rank(128), rank_whole = rank(head_dim == 128 ? 256 : 128);
@@ -76,11 +76,9 @@ inline CrossShape cross_shape(long rows, int batch, long streams, int columns, l
     const double even = n / kCus * 0.4 * 0.42 * tiles + 0.21 * tiles;
     whole = 9 + (even > 0.9 * tiles ? even : 0.9 * tiles);
   } else {
-    whole = 0;
-    for (long left = found; left > 0; left -= 3 * kCus) {
-      const long on_cu = left >= 3 * kCus ? 3 : ceil_div(left, kCus);
-      whole += (0.42 * on_cu > 0.9 ? 0.42 * on_cu : 0.9) * tiles + 9;
-    }
+    const long full = found / (3 * kCus), left = ceil_div(found % (3 * kCus), kCus);  // rounds of three workgroups a CU, and the last
+    whole = full * (3 * 0.42 * tiles + 9);
+    if (left > 0) whole += (0.42 * left > 0.9 ? 0.42 * left : 0.9) * tiles + 9;
   }
   s.halves = span(n, 0.55 * tiles, 10, rank_halves) <= whole;
   s.ranked = s.halves ? rank_halves : rank_whole;

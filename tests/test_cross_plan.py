@@ -1,0 +1,64 @@
+"""The choices of cross_plan.h, compiled for the host: bounds that hold for any hints, and both sides of the rules."""
+import os
+import random
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+CSRC = os.path.join(HERE, "..", "paper_2507_11830_amd", "csrc")
+
+
+@pytest.fixture(scope="module")
+def shape(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("plan") / "cross_plan")
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-Wno-unused-function", "-Wno-unknown-pragmas", "-fsanitize=undefined", "-fno-sanitize-recover=all",
+                           "-I", CSRC, os.path.join(HERE, "cross_plan_host.cpp"), "-o", exe])
+
+    def ask(lines):
+        out = subprocess.run([exe], input="\n".join(" ".join(str(int(x)) for x in l) for l in lines), capture_output=True, text=True, check=True).stdout
+        return [tuple(int(x) for x in l.split()) for l in out.splitlines()]
+
+    return ask
+
+
+def hints(heads, batch, total_q, max_q, max_kv, can_cut=True):
+    hq, hkv, d = heads
+    group, cols = hq // hkv, 1
+    while group & (group - 1) == 0 and cols < group and cols < 32:
+        cols *= 2
+    return total_q * hq, batch, batch * (hq // cols), cols, total_q, max_q, max_kv, d, can_cut
+
+
+def test_any_hints(shape):
+    rng = random.Random(1)
+    big = lambda: int(2 ** rng.uniform(0, 31)) - 1
+    lines = []
+    for _ in range(4000):
+        heads = rng.choice([(8, 1, 128), (32, 8, 128), (12, 3, 64), (1, 1, 64), (65536, 1, 128), (7, 7, 64)])
+        lines.append(hints(heads, max(1, big()), max(1, big()), max(1, big()), big(), rng.random() < 0.8))
+    for line, (halves, ranked, pieces) in zip(lines, shape(lines)):
+        rows, batch, streams, cols, total_q, max_q, max_kv, d, can_cut = line
+        assert 1 <= pieces <= 16 and (can_cut or pieces == 1)
+        if pieces > 1:
+            assert halves and pieces * rows <= 1 << 17  # what a workspace is sized for
+            assert 2 * pieces <= -(-max_kv // 64)  # two key tiles each, one for either wave group
+            assert pieces * max(rows // 128, streams) <= 256  # one round
+        if batch == 1:
+            assert not ranked
+
+
+@pytest.mark.parametrize("heads,batch,total_q,max_q,max_kv,want", [
+    ((8, 1, 128), 8, 8 * 4096, 4096, 4096, (0, 0, 1)),  # one length: whole tiles by order
+    ((8, 1, 128), 1, 40, 40, 9000, (1, 0, None)),  # few queries on many keys: pieces
+    ((8, 1, 128), 1, 40, 40, 500, (1, 0, 1)),  # little to cut
+    ((32, 4, 128), 1, 1137, 1137, 4580, (0, 0, 1)),  # halves would be a second round for a tenth of them
+    ((32, 8, 128), 9, 9 * 254, 254, 2133, (1, 0, 1)),
+    ((16, 2, 64), 8, 4500, 1089, 1891, (0, 1, 1)),  # uneven, more than a round: longest first
+], ids=str)
+def test_both_sides(shape, heads, batch, total_q, max_q, max_kv, want):
+    (halves, ranked, pieces), = shape([hints(heads, batch, total_q, max_q, max_kv)])
+    assert (halves, ranked) == want[:2]
+    assert pieces == want[2] if want[2] else pieces >= 4
+    (halves, ranked, pieces), = shape([hints(heads, batch, total_q, max_q, max_kv, False)])
+    assert pieces == 1

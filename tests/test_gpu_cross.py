@@ -228,3 +228,31 @@ def test_captured(nq, nk):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(want.view(torch.int16), c.out.view(torch.int16))
+
+
+def test_pages_beyond_four_gigabytes():
+    """A pool whose last pages lie past 32-bit byte offsets, for the calls that write and read it."""
+    heads, pages = 8, 140_000  # 4.6 GB each for K and V
+    cache = sp.KVCache(*(torch.empty(pages, heads, 16, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    nk, nq = [70, 33], [5, 40]
+    far = torch.tensor([[pages - 1, pages - 7, pages - 3, pages - 2, pages - 9], [pages - 20, 3, pages - 21, -1, -1]], dtype=torch.int32, device="cuda")
+    near = torch.tensor([[0, 1, 2, 4, 5], [6, 7, 8, -1, -1]], dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(103, heads, 128, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    cu_k, zero = torch.tensor([0, 70, 103], dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    sp.sp_norm_rope_append(cache, None, k, v, None, cu_k, zero, far)
+    for pool, x in ((cache.k_pages, k), (cache.v_pages, v)):
+        assert torch.equal(pool[pages - 9, :, 5].view(torch.int16), x[69].view(torch.int16))
+    q = torch.randn(45, 8, 128, generator=g, device="cuda").to(torch.bfloat16)
+    cu, lens = torch.tensor([0, 5, 45], dtype=torch.int32, device="cuda"), torch.tensor(nk, dtype=torch.int32, device="cuda")
+    src, dst = far.flatten()[[0, 1, 2, 3, 4, 5, 7]], near.flatten()[[0, 1, 2, 3, 4, 5, 7]]
+    sp.sp_pages_copy(cache, src, dst)
+    near[1, 1] = 3
+    outs = []
+    for table in (far, near):
+        outs.append(torch.empty_like(q))
+        sp.sp_attn_cross(cache, q, outs[-1], cu, lens, table, 40, 70, 0.09)
+    assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16)) and torch.isfinite(outs[0]).all()
+    sp.sp_pages_copy(cache, dst, src)  # and back over the boundary
+    sp.sp_attn_cross(cache, q, outs[1], cu, lens, far, 40, 70, 0.09)
+    assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
