@@ -5,8 +5,8 @@
 // Times are estimated in us from constants that leave the least behind on 960 batches drawn at random (eight head shards, 1 to 24
 // sequences, up to 1600 workgroups of 128 columns, 20 to 8192 keys; equal lengths, unequal ones of both sides, unequal keys only;
 // all forms timed): 2.3 % over the best form of each batch, where the causal rules leave 7 %.  Both sides of it: 1 x 1137
-// queries on 4580 keys at 32q/4kv in halves 112 us (a second round of workgroups for the last tenth), whole tiles 88; 9 x 254 on 2133 at
-// 32q/8kv 98 and 107; 12 x 17..600 on 65..2500 at 12q/3kv, head_dim 64, 27 and 38.
+// queries on 4580 keys at 32q/4kv in halves 112 us (a second round of workgroups for the last tenth), whole tiles 88; 2 x 206 on 2284 at
+// 16q/2kv 28 and 44; 12 x 17..600 on 65..2500 at 12q/3kv, head_dim 64, 27 and 38.
 #pragma once
 #include "cut_plan.h"
 
