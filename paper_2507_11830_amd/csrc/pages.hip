@@ -6,8 +6,8 @@
 // per page of the pool, but nothing orders one workgroup of the scan behind another, every workgroup of the
 // second launch finds its pages by itself, and the result does not depend on timing.
 //
-// Launches: reserve and fork two (scan and plan; apply), compact three (scan; ranks; apply), release and copy one.  All but
-// the copy are bound by their chains of memory round trips, the copy by HBM.
+// Launches: reserve and fork two (scan and plan; apply), compact three (scan; ranks; apply), each one on small pools; release and
+// copy one.  All but the copy are bound by their chains of memory round trips, the copy by HBM.
 #include "attn_tile.h"
 
 namespace sp {
@@ -131,6 +131,20 @@ __global__ __launch_bounds__(kPageThreads) void pages_scan_kernel(PagesArgs p) {
   }
 }
 
+// The free pages of 64 words, one per lane, that are number 0 .. m - 1 from some page on: take(k, page).  rank: number of the word's
+// first one; page0: first page of lane 0's word.  A word at a time, a lane per page: a lane that went through its own word would
+// skip the pages before number 0 one by one (64 entries of a few pages each: 55 us a pass of fork and reserve, 24 so).
+template <typename Take>
+static __device__ __forceinline__ void take_words(uint64_t bits, int rank, int page0, int m, Take take) {
+  const int lane = threadIdx.x & 63, n = __builtin_popcountll(bits);
+  for (uint64_t words = __builtin_amdgcn_ballot_w64(n > 0 && rank < m && rank + n > 0); words != 0; words &= words - 1) {
+    const int l = __builtin_ctzll(words);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)bits, l), hi = __builtin_amdgcn_readlane((uint32_t)(bits >> 32), l);
+    const int k = __builtin_amdgcn_readlane(rank, l) + __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+    if (((lane < 32 ? lo >> lane : hi >> (lane - 32)) & 1) != 0 && k >= 0 && k < m) take(k, page0 + 64 * l + lane);
+  }
+}
+
 // Which segments hold the pool's free pages number `first` and on.  seg_before[q]: free pages before segment s0 + q, for the
 // kPageThreads segments from s0 on.
 struct FreePages {
@@ -160,12 +174,9 @@ struct FreePages {
           else lo = mid + 1;
         }
         for (int q = lo + w; q < kPageThreads && s0 + q < p.nseg && seg_before[q] < first + m; q += kPageWaves) {
-          uint64_t bits = p.free_bits[(long)(s0 + q) * kSegWords + lane];
+          const uint64_t bits = p.free_bits[(long)(s0 + q) * kSegWords + lane];
           const int mine = __builtin_popcountll(bits);
-          int k = seg_before[q] + lane_prefix(mine) - mine - first;
-          const int page = (s0 + q) * kSegment + 64 * lane;
-          for (; bits != 0 && k < m; bits &= bits - 1, ++k)
-            if (k >= 0) take(k, page + __builtin_ctzll(bits));
+          take_words(bits, seg_before[q] + lane_prefix(mine) - mine - first, (s0 + q) * kSegment, m, take);
         }
       }
       const int next = s0 + kPageThreads;
@@ -238,16 +249,16 @@ __global__ __launch_bounds__(kPageThreads) void pages_take_kernel(PagesArgs p) {
   }
 }
 
-// Few entries on a small pool: scan, plan and entries in one workgroup, a wave per entry, so one launch instead of two.  Of several
+// Few entries on a small pool: scan, plan and entries in one workgroup, up to four entries a wave, so one launch instead of two.  Of several
 // entries for one child the first is taken, and entries for one row get their room one after the other.
-constexpr int kSmallWaves = 16, kSmallPages = kSmallWaves * 1024, kSmallWidth = 1024;
+constexpr int kSmallWaves = 16, kSmallEntries = 64, kSmallPages = kSmallWaves * 1024, kSmallWidth = 1024;
 
 template <int OP>
 __global__ __launch_bounds__(64 * kSmallWaves) void pages_small_kernel(PagesArgs p) {
   constexpr int PER = 16;                               // words of a wave
   constexpr int WORDS = kSmallWaves * PER, LANE = WORDS / 64;
   __shared__ uint64_t s_bits[WORDS];
-  __shared__ int s_a[kSmallWaves], s_b[kSmallWaves], s_size[kSmallWaves], s_first[kSmallWaves + 1];
+  __shared__ int s_a[kSmallEntries], s_b[kSmallEntries], s_size[kSmallEntries], s_first[kSmallEntries + 1];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int refs[PER];
 #pragma unroll
@@ -284,55 +295,55 @@ __global__ __launch_bounds__(64 * kSmallWaves) void pages_small_kernel(PagesArgs
   if (lane < PER) s_bits[w * PER + lane] = mine;
   __syncthreads();
   if (w >= p.n) return;
-  // every wave by itself: its entry, and the free pages before each of the lane's words
+  // every wave by itself: its entries, and the free pages before each of the lane's words
   uint64_t bits[LANE];
-  int count = 0;
+  int before[LANE], all_free = 0;
 #pragma unroll
   for (int i = 0; i < LANE; ++i) {
-    bits[i] = s_bits[LANE * lane + i];
-    count += __builtin_popcountll(bits[i]);
+    bits[i] = s_bits[64 * i + lane];
+    const int count = __builtin_popcountll(bits[i]), incl = wave_scan_incl(count);
+    before[i] = all_free + incl - count;
+    all_free += __builtin_amdgcn_readlane(incl, 63);
   }
-  const int incl = wave_scan_incl(count), all_free = __builtin_amdgcn_readlane(incl, 63);
   const int missing = max(s_first[p.n] - all_free, 0);
   if (w == 0 && lane == 0) *p.shortfall = missing;
-  const int a = s_a[w], b = s_b[w], size = s_size[w], first = s_first[w], need = s_first[w + 1] - first;
-  auto take_pages = [&](auto take) __attribute__((always_inline)) {
-    int k = incl - count - first;
+  for (int e = w; e < p.n; e += kSmallWaves) {
+    const int a = s_a[e], b = s_b[e], size = s_size[e], first = s_first[e], need = s_first[e + 1] - first;
+    auto take_pages = [&](auto take) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < LANE; ++i)
-      for (uint64_t left = bits[i]; left != 0 && k < need; left &= left - 1, ++k)
-        if (k >= 0) take(k, 64 * (LANE * lane + i) + __builtin_ctzll(left));
-  };
-  if constexpr (OP == kReserve) {
-    if (missing > 0 || size == 0) return;
-    if (lane == 0) atomicMax(p.lens + a, b);
-    int32_t *row = p.table + (long)a * p.max_pages + size - need;
-    take_pages([&](int k, int page) __attribute__((always_inline)) {
-      row[k] = page;
-      p.refs[page] = 1;
-    });
-  } else {
-    const bool taken = missing == 0 && size >= 0;
-    if (!(taken && need > 0) && lane == 0) {
-      p.copy_src[w] = p.copy_dst[w] = -1;
-      p.copy_rows[w] = 0;
-    }
-    if (!taken || size == 0) return;
-    const int32_t *from = p.table + (long)a * p.max_pages;
-    int32_t *to = p.table + (long)b * p.max_pages;
-    const int full = size / kPage;
-    if (lane == 0) p.lens[b] = size;
-    take_pages([&](int, int page) __attribute__((always_inline)) {
-      p.copy_src[w] = from[full];
-      p.copy_dst[w] = page;
-      p.copy_rows[w] = size % kPage;
-      to[full] = page;
-      p.refs[page] = 1;
-    });
-    for (int c = lane; c < full; c += 64) {
-      const int page = from[c];
-      to[c] = page;
-      if (page >= 0 && page < p.num_pages) atomicAdd(p.refs + page, 1);
+      for (int i = 0; i < LANE; ++i) take_words(bits[i], before[i] - first, 64 * 64 * i, need, take);
+    };
+    if constexpr (OP == kReserve) {
+      if (missing > 0 || size == 0) continue;
+      if (lane == 0) atomicMax(p.lens + a, b);
+      int32_t *row = p.table + (long)a * p.max_pages + size - need;
+      take_pages([&](int k, int page) __attribute__((always_inline)) {
+        row[k] = page;
+        p.refs[page] = 1;
+      });
+    } else {
+      const bool taken = missing == 0 && size >= 0;
+      if (!(taken && need > 0) && lane == 0) {
+        p.copy_src[e] = p.copy_dst[e] = -1;
+        p.copy_rows[e] = 0;
+      }
+      if (!taken || size == 0) continue;
+      const int32_t *from = p.table + (long)a * p.max_pages;
+      int32_t *to = p.table + (long)b * p.max_pages;
+      const int full = size / kPage;
+      if (lane == 0) p.lens[b] = size;
+      take_pages([&](int, int page) __attribute__((always_inline)) {
+        p.copy_src[e] = from[full];
+        p.copy_dst[e] = page;
+        p.copy_rows[e] = size % kPage;
+        to[full] = page;
+        p.refs[page] = 1;
+      });
+      for (int c = lane; c < full; c += 64) {
+        const int page = from[c];
+        to[c] = page;
+        if (page >= 0 && page < p.num_pages) atomicAdd(p.refs + page, 1);
+      }
     }
   }
 }
@@ -412,6 +423,89 @@ __global__ __launch_bounds__(kPageThreads) void pages_rank_kernel(PagesArgs p) {
       p.rank[page] = r;
       p.moved_refs[r] = refs[i];
     }
+  }
+}
+
+// Compaction of a small pool with a small table in one launch: what the three do, in one workgroup.  New counts and entries are written
+// when all old ones have been read, as both may be the table's own arrays.
+constexpr int kSmallTable = 16 * 1024;  // entries
+
+__global__ __launch_bounds__(64 * kSmallWaves) void pages_compact_small_kernel(PagesArgs p) {
+  constexpr int PER = 16, WORDS = kSmallWaves * PER, LANE = WORDS / 64;
+  __shared__ uint64_t s_bits[WORDS];
+  __shared__ int s_before[WORDS];                      // free pages before a word
+  __shared__ int s_refs[kSmallPages / 2];              // of the i-th page that moves: its count,
+  __shared__ uint16_t s_dst[kSmallPages / 2];          // and where it goes
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int entries = p.num_rows * p.max_pages;  // at most kSmallTable
+  int refs[PER], entry[kSmallTable / (64 * kSmallWaves)], len[kSmallTable / (64 * kSmallWaves)];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) refs[i] = p.refs[min(1024 * w + 64 * i + lane, p.num_pages - 1)];
+#pragma unroll
+  for (int i = 0; i < kSmallTable / (64 * kSmallWaves); ++i) {
+    const int at = 1024 * i + threadIdx.x;
+    entry[i] = len[i] = 0;
+    if (1024 * i >= entries) continue;  // uniform
+    entry[i] = p.table[min(at, entries - 1)];
+    len[i] = p.lens[min(at, entries - 1) / p.max_pages];
+  }
+  uint64_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint64_t bits = __builtin_amdgcn_ballot_w64(refs[i] <= 0 && 1024 * w + 64 * i + lane < p.num_pages);
+    if (lane == i) mine = bits;
+  }
+  if (lane < PER) s_bits[w * PER + lane] = mine;
+  __syncthreads();
+  if (w == 0) {
+    int c[LANE], count = 0;
+#pragma unroll
+    for (int i = 0; i < LANE; ++i) {
+      c[i] = count;
+      count += __builtin_popcountll(s_bits[LANE * lane + i]);
+    }
+    const int before = wave_scan_incl(count) - count;
+#pragma unroll
+    for (int i = 0; i < LANE; ++i) s_before[LANE * lane + i] = before + c[i];
+  }
+  __syncthreads();
+  auto free_before = [&](int page) __attribute__((always_inline)) {  // page < kSmallPages
+    return s_before[page >> 6] + __builtin_popcountll(s_bits[page >> 6] & ((1ull << (page & 63)) - 1));
+  };
+  auto is_free = [&](int page) __attribute__((always_inline)) { return ((s_bits[page >> 6] >> (page & 63)) & 1) != 0; };
+  const int used = p.num_pages - s_before[WORDS - 1] - __builtin_popcountll(s_bits[WORDS - 1]);
+  const int holes = used < kSmallPages ? free_before(used) : 0;
+  auto mover = [&](int page) __attribute__((always_inline)) { return page - free_before(page) - (used - holes); };
+  if (threadIdx.x == 0) {
+    p.moved[0] = holes;
+    p.moved[1] = used;
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int page = 1024 * w + 64 * i + lane;
+    if (page >= p.num_pages || holes == 0) continue;
+    if (page < used && is_free(page)) {
+      const int r = free_before(page);
+      s_dst[r] = (uint16_t)page;
+      p.move_dst[r] = page;
+    } else if (page >= used && !is_free(page)) {
+      const int r = mover(page);
+      s_refs[r] = refs[i];
+      p.move_src[r] = page;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int page = 1024 * w + 64 * i + lane;
+    if (page < p.num_pages) p.new_refs[page] = page >= used ? 0 : is_free(page) ? s_refs[free_before(page)] : refs[i];
+  }
+#pragma unroll
+  for (int i = 0; i < kSmallTable / (64 * kSmallWaves); ++i) {
+    const int at = 1024 * i + threadIdx.x;
+    if (at >= entries || at % p.max_pages >= pages_of(len[i])) continue;
+    const int page = entry[i];
+    p.new_table[at] = page >= used && page < p.num_pages && !is_free(page) ? s_dst[mover(page)] : page;
   }
 }
 
@@ -512,10 +606,12 @@ static int launched(const char *what) {
   return e == hipSuccess ? SP_OK : fail(SP_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
 }
 
-// Scan and take, or both in one launch: 4 forks of a row of 19 pages in a pool of 160 6.7 us (kernels alone) as two launches.
+// Scan and take, or both in one launch where one workgroup is quick enough: up to an entry a wave, or rows that are short together.  A
+// pass of release, fork, copy and reserve: 4 forks of a row of 19 pages 24.8 us with two launches each, 18.4 with one; 41 of up to 12
+// 26 and 21; but 52 of 212 pages 27 and 40.
 template <int OP>
 static void launch_take(const PagesArgs &p, hipStream_t stream) {
-  if (p.n <= kSmallWaves && p.num_pages <= kSmallPages && p.max_pages <= kSmallWidth) {
+  if (p.num_pages <= kSmallPages && p.max_pages <= kSmallWidth && (p.n <= kSmallWaves || (p.n <= kSmallEntries && (long)p.n * p.max_pages <= 4096))) {
     hipLaunchKernelGGL(pages_small_kernel<OP>, dim3(1), dim3(64 * kSmallWaves), 0, stream, p);
     return;
   }
@@ -561,6 +657,10 @@ int launch_pages_compact(const sp_page_table &t, int32_t *new_block_table, int32
   p.move_src = move_src;
   p.move_dst = move_dst;
   p.moved = moved;
+  if (t.num_pages <= kSmallPages && (long)t.num_rows * t.max_pages_per_seq <= kSmallTable) {
+    hipLaunchKernelGGL(pages_compact_small_kernel, dim3(1), dim3(64 * kSmallWaves), 0, stream, p);
+    return launched("sp_pages_compact");
+  }
   const int count_groups = (int)min((long)1024, ((long)t.num_pages + kPageThreads - 1) / kPageThreads);
   hipLaunchKernelGGL(pages_scan_kernel<kCompact>, dim3(p.nseg), dim3(kPageThreads), 0, stream, p);
   hipLaunchKernelGGL(pages_rank_kernel, dim3(p.nseg), dim3(kPageThreads), 0, stream, p);

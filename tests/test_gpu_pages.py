@@ -137,7 +137,7 @@ class Both:
         return a, b, moved
 
 
-@pytest.mark.parametrize("pad", (0, 30), ids=("short-lists", "long-lists"))
+@pytest.mark.parametrize("pad", (0, 70), ids=("short-lists", "long-lists"))
 @pytest.mark.parametrize("pages", (1, 2, 63, 64, 65, 300, 1023, 1025, 4095, 4096, 4097, 9000, 16383, 16384, 16385))
 def test_random_lives(pages, pad):
     rng = np.random.default_rng(pages)
@@ -193,7 +193,7 @@ def test_a_pool_larger_than_one_round_of_segments():
     assert int(b.t.ref_counts[:used].min()) == 1 and int(b.t.ref_counts[used:].abs().max()) == 0
 
 
-@pytest.mark.parametrize("pad", (0, 30))
+@pytest.mark.parametrize("pad", (0, 70))
 def test_all_or_nothing(pad):
     b = Both(6, 8, 10, pad)
     b.reserve([0, 1], [100, 20])  # 7 + 2 pages: one is left
@@ -206,13 +206,30 @@ def test_all_or_nothing(pad):
 
 
 def test_lists_up_to_the_small_kernel_s_length():
-    for n in (1, 15, 16, 17):
-        b = Both(64, 40, 3000)
-        b.reserve(np.arange(n), 600 - 30 * np.arange(n))
-        b.fork(np.arange(n)[::-1], 20 + np.arange(n))
-        b.reserve(20 + np.arange(n), [640] * n)
-        b.fork([3, 40], [40, 41])  # the second parent is empty when the call is made
-        b.release(np.arange(64))
+    for n in (1, 15, 16, 17, 33, 63, 64, 65):
+        b = Both(140, 40, 6000)
+        b.reserve(np.arange(n), 640 - 9 * np.arange(n))
+        b.fork(np.arange(n)[::-1], 70 + np.arange(n))
+        b.reserve(70 + np.arange(n), [640] * n)
+        b.fork([0, 136], [136, 137])  # the second parent is empty when the call is made
+        b.compact(in_place=n % 2 == 1)
+        b.release(np.arange(140))
+
+
+@pytest.mark.parametrize("rows,width", [(16, 1024), (128, 128), (1, 3000), (17, 1024), (1, 0), (0, 5)])
+def test_compaction_of_small_and_large_tables(rows, width):
+    """Up to 16384 entries and pages in one launch."""
+    rng = np.random.default_rng(rows)
+    for pages in (900, 16384, 16385):
+        b = Both(rows, width, pages)
+        if rows * width:
+            n = min(rows, 12)
+            b.reserve(np.arange(n), np.minimum(16 * width, rng.integers(1, 16 * pages // n // 2, n)))
+            b.release([0, n // 2], [5, 40])
+            b.reserve([n - 1], [16 * min(width, 20)])
+            b.release([0])
+        b.compact(in_place=pages == 900)
+        b.compact(in_place=True)  # nothing left to move
 
 
 def test_wide_tables():
@@ -233,7 +250,7 @@ def test_lists_longer_than_a_workgroup():
     b.compact(in_place=False)
 
 
-@pytest.mark.parametrize("pad", (0, 30))
+@pytest.mark.parametrize("pad", (0, 70))
 def test_skipped_entries(pad):
     b = Both(5, 4, 40, pad)
     b.reserve([0, -1, 7, 1, 2], [33, 16, 16, 65, 64])  # rows outside the table, more than a row holds
@@ -241,9 +258,9 @@ def test_skipped_entries(pad):
     b.release([-1, 5, 3], [1, 1, 1])
 
 
-@pytest.mark.parametrize("pad", (0, 30))
+@pytest.mark.parametrize("pad", (0, 70))
 def test_the_same_row_twice(pad):
-    b, none = Both(4, 8, 64), [-1] * pad
+    b, none = Both(4, 8, 64, pad), [-1] * pad
     sp.sp_pages_reserve(b.t, dev([1, 1, 1, *none]), dev([40, 100, 70, *none]), b.short, b.ws)
     sp.sp_debug_validate_pages(b.t)
     assert b.t.seq_lens.tolist() == [0, 100, 0, 0] and int(b.t.ref_counts.sum()) == 7
