@@ -12,6 +12,7 @@
 //   - chunks of a few tokens, one column tile of a wave: the decode kernel with equal shares or fixed splits (75 batches of
 //     1 to 200 such chunks on 20 to 8000 keys: 22 % faster than query tiles in the mean).  With two column tiles, as in the causal calls,
 //     it took 13 % longer than query tiles in pieces (75 batches);
+//   - few keys, up to 256: they stay in LDS while a workgroup goes through many queries (attn_cross_resident.hip);
 //   - otherwise query tiles of 256 columns (128 at head_dim 64, several workgroups a CU), or of 128 columns whose two wave groups take
 //     alternate key tiles, and where even these leave most CUs idle, in pieces of the key range.
 #include "decode_stream.h"
@@ -88,9 +89,17 @@ static CrossShape shape_of(int batch, int total_q, int max_q_len, int max_kv_len
   return s;
 }
 
+static CrossResident resident_of(int batch, int total_q, int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim) {
+  const PrefillTuning tune = prefill_tuning();
+  if (tune.split != 0 || tune.kv_splits != 0 || tune.order != 0) return {0, 0, 0};  // the caller asks for query tiles
+  const int gshift = column_shift(num_q_heads / num_kv_heads);
+  return cross_resident((long)total_q * num_q_heads, (long)batch * (num_q_heads >> gshift), 1 << gshift, max_q_len, max_kv_len, head_dim);
+}
+
 size_t cross_workspace_bytes(int batch, int total_q, int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim) {
   const long rows = (long)total_q * num_q_heads;
-  const int kvs = shape_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim, true).pieces;
+  const bool resident = resident_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim).blocks > 0;
+  const int kvs = resident ? 1 : shape_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim, true).pieces;
   const size_t pieces = kvs > 1 ? (size_t)rows * kvs * (head_dim + 2) * sizeof(float) : 0;
   const size_t few = prefill_tuning().short_chunk == 1 || max_q_len > decode_route_cap(num_q_heads, num_kv_heads) ? 0 : decode_multi_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim);
   return pieces > few ? pieces : few;
@@ -127,6 +136,8 @@ int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t
   a.batch = batch;
   a.total_q = total_q;
   const long rows = (long)total_q * num_q_heads;
+  const CrossResident resident = resident_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, c.num_kv_heads, c.head_dim);
+  if (resident.blocks > 0) return launch_cross_resident(a, resident, c.head_dim, batch, max_q_len, stream);
   CrossShape shape = shape_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, c.num_kv_heads, c.head_dim, workspace != nullptr);
   int kvs = shape.pieces;
   const size_t fit = workspace_bytes / ((size_t)rows * (c.head_dim + 2) * sizeof(float));

@@ -41,6 +41,28 @@ inline int cross_piece_count(long rows, long wgs, long max_kv_len, int head_dim)
   return best;
 }
 
+// Keys that stay in LDS (attn_cross_resident.hip), 32 per block: two workgroups of four waves a CU where both fit, else one of eight, in
+// one round of workgroups.  Up to 128 keys (520 batches of 9 to 5000 queries: 1.3 times as fast as query tiles at head_dim 64 in the
+// mean, 1.7 at 128, five of them slower; 14 x 1844 queries on 129 at 32q/8kv 252 us in tiles, 137 so); up to 256 where there are enough
+// queries (8 x 1749 on 229 at 16q/2kv 74 and 59, but 1 x 78 on 251 at 8q/1kv 11.7 and 16).  Beyond, the weights are the work: 4 x 73
+// on 422 at 16q/2kv, head_dim 64, 8.9 and 14.5.
+constexpr int kResidentLds = 128 * 1024;
+struct CrossResident {
+  int blocks;  // 0: not taken
+  int waves;
+  int rounds;  // of 32 columns per wave
+};
+inline CrossResident cross_resident(long rows, long streams, int columns, long max_q_len, long max_kv_len, int head_dim) {
+  CrossResident r = {0, 0, 0};
+  if (max_kv_len < 1 || max_kv_len > 256 || (max_kv_len > 128 && rows < 48000) || max_q_len > (1 << 24) || streams > 0x7fffffffL) return r;
+  const long blocks = ceil_div(max_kv_len, 32), lds = blocks * 2 * 32 * head_dim * 2;
+  r.waves = 2 * lds <= kResidentLds ? 4 : 8;
+  const long wgs = (r.waves == 4 ? 2 : 1) * kCus, rounds = ceil_div(rows, 32 * r.waves * wgs);
+  r.rounds = (int)(rounds < 1 ? 1 : rounds > 16 ? 16 : rounds);
+  if (ceil_div(max_q_len * columns, 32 * r.waves * r.rounds) <= 65535) r.blocks = (int)blocks;
+  return r;
+}
+
 // columns: query columns of a token (heads that share a KV head's column dimension); streams: sequences x head groups.
 inline CrossShape cross_shape(long rows, int batch, long streams, int columns, long total_q, long max_q_len, long max_kv_len, int head_dim,
                               bool can_cut) {

@@ -607,7 +607,7 @@ static int launched(const char *what) {
 }
 
 // Scan and take, or both in one launch where one workgroup is quick enough: up to an entry a wave, or rows that are short together.  A
-// pass of release, fork, copy and reserve: 4 forks of a row of 19 pages 24.8 us with two launches each, 18.4 with one; 41 of up to 12
+// pass of release, fork, copy and reserve: 4 forks of a row of 19 pages 24.8 us with two launches each, 18.4 with one; 41 of up to 17
 // 26 and 21; but 52 of 212 pages 27 and 40.
 template <int OP>
 static void launch_take(const PagesArgs &p, hipStream_t stream) {

@@ -1464,6 +1464,9 @@ inline int launch_cfg(void (*fn)(Args), bool *attr_set, size_t smem, int cols, c
 int launch_prefill_cut(const PrefillArgs &a, int head_dim, int batch, int max_q_len, int groups, hipStream_t stream);
 // attn_prefill_fresh.hip: append and prefill in one launch; split: 128-column workgroups.
 int launch_prefill_fresh(const FreshArgs &a, bool split, int head_dim, int batch, int max_q_len, hipStream_t stream);
+// attn_cross_resident.hip: without a mask, on keys that stay in LDS.
+struct CrossResident;
+int launch_cross_resident(const CrossArgs &a, const CrossResident &plan, int head_dim, int batch, int max_q_len, hipStream_t stream);
 struct DecodeArgs;
 // attn_mixed.hip: ranked prefill workgroups of 128 (split) or 256 columns and `shares` workgroups of the equal-share decode.
 int launch_mixed(const PrefillArgs &a, const DecodeArgs &d, int shares, int pieces, bool split, int head_dim, int batch, int max_q_len, hipStream_t stream);

@@ -36,8 +36,8 @@ def test_any_hints(shape):
     lines = []
     for _ in range(4000):
         heads = rng.choice([(8, 1, 128), (32, 8, 128), (12, 3, 64), (1, 1, 64), (65536, 1, 128), (7, 7, 64)])
-        lines.append(hints(heads, max(1, big()), max(1, big()), max(1, big()), big(), rng.random() < 0.8))
-    for line, (halves, ranked, pieces) in zip(lines, shape(lines)):
+        lines.append(hints(heads, max(1, big()), max(1, big()), max(1, big()), big() if rng.random() < 0.7 else rng.randint(0, 300), rng.random() < 0.8))
+    for line, (halves, ranked, pieces, blocks, waves, rounds) in zip(lines, shape(lines)):
         rows, batch, streams, cols, total_q, max_q, max_kv, d, can_cut = line
         assert 1 <= pieces <= 16 and (can_cut or pieces == 1)
         if pieces > 1:
@@ -46,6 +46,9 @@ def test_any_hints(shape):
             assert pieces * max(rows // 128, streams) <= 256  # one round
         if batch == 1:
             assert not ranked
+        if blocks > 0:  # all keys fit LDS, twice on a CU with four waves; the grid holds all columns
+            assert 32 * blocks >= max_kv and blocks * 128 * d * (2 if waves == 4 else 1) <= 128 * 1024 and waves in (4, 8) and 1 <= rounds <= 16
+            assert max_kv <= 256 and -(-max_q * cols // (32 * waves * rounds)) <= 65535 and streams < 2**31
 
 
 @pytest.mark.parametrize("heads,batch,total_q,max_q,max_kv,want", [
@@ -57,8 +60,16 @@ def test_any_hints(shape):
     ((16, 2, 64), 8, 4500, 1089, 1891, (0, 1, 1)),  # uneven, more than a round: longest first
 ], ids=str)
 def test_both_sides(shape, heads, batch, total_q, max_q, max_kv, want):
-    (halves, ranked, pieces), = shape([hints(heads, batch, total_q, max_q, max_kv)])
+    (halves, ranked, pieces, blocks, _, _), = shape([hints(heads, batch, total_q, max_q, max_kv)])
+    assert blocks == 0
     assert (halves, ranked) == want[:2]
     assert pieces == want[2] if want[2] else pieces >= 4
-    (halves, ranked, pieces), = shape([hints(heads, batch, total_q, max_q, max_kv, False)])
-    assert pieces == 1
+    assert shape([hints(heads, batch, total_q, max_q, max_kv, False)])[0][2] == 1
+
+
+@pytest.mark.parametrize("heads,total_q,max_kv,want", [
+    ((8, 1, 128), 57, 10, (1, 4, 1)), ((32, 8, 128), 43303, 18, (1, 4, 16)), ((8, 1, 128), 78, 128, (4, 4, 1)), ((8, 1, 128), 78, 129, (0,)),
+    ((16, 2, 128), 13992, 229, (8, 8, 4)), ((16, 2, 64), 13992, 256, (8, 4, 4)), ((16, 2, 64), 13992, 257, (0,)), ((16, 2, 64), 100, 0, (0,)),
+], ids=str)
+def test_keys_that_stay_in_lds(shape, heads, total_q, max_kv, want):
+    assert shape([hints(heads, 1, total_q, total_q, max_kv)])[0][3:3 + len(want)] == want

@@ -139,6 +139,34 @@ def test_kernels_behind_it(heads, nq, nk):
     assert torch.equal(first.view(torch.int16), c.out.view(torch.int16))  # the same bits again
 
 
+@pytest.mark.parametrize("heads,nq,nk", [
+    ((8, 1, 128), [300, 7, 0, 65], [64, 1, 30, 0]),
+    ((8, 1, 128), [5000, 10, 40], [128, 97, 0]),
+    ((32, 8, 128), [1500, 33, 600], [256, 129, 31]),  # more than 128 keys: one workgroup a CU
+    ((12, 3, 64), [200, 500], [32, 33]),
+    ((16, 2, 64), [4000, 1], [200, 255]),
+    ((7, 1, 64), [50, 3], [33, 100]),
+    ((71, 1, 64), [9, 40], [1, 2]),
+    ((2, 2, 128), [33, 31, 32], [63, 64, 65]),
+    ((64, 1, 128), [300, 2], [16, 17]),
+], ids=lambda x: "x".join(map(str, x[:3])))
+def test_keys_that_stay_in_lds(heads, nq, nk):
+    c = Case(heads, nq, nk, seed=3)
+    assert c.workspace() is None or max(nq) * heads[0] // heads[1] <= 32
+    c.call(None)
+    c.check()
+    first = c.out.clone()
+    grids = kernel_launches(lambda: c.call(None))
+    assert len(grids) == 1 and grids[0][1][0] == (256 if max(nk) <= 128 or heads[2] == 64 else 512)
+    c.lens.copy_(torch.clamp(c.lens - 1, min=0))  # shorter than the hint says
+    c.nk = np.maximum(c.nk - 1, 0)
+    c.call(None)
+    c.check()
+    c.lens += 1000  # and longer: no more than the hint, in memory
+    c.call(None)
+    assert first.shape == c.out.shape
+
+
 def test_the_division_of_the_keys_is_taken():
     """Few query tokens on long ranges: pieces and their merge; and with less workspace than asked for, fewer or none."""
     c = Case((8, 1, 128), [40], [9000], seed=1)
@@ -208,7 +236,7 @@ def test_sub_ranges_and_padded_buffers():
     assert torch.isnan(few.out[:4]).all() and torch.isnan(few.out[8:]).all()
 
 
-@pytest.mark.parametrize("nq,nk", [([1] * 8, [900] * 8), ([70, 3], [5000, 200]), ([2000], [1500])], ids=("tokens", "pieces", "tiles"))
+@pytest.mark.parametrize("nq,nk", [([1] * 8, [900] * 8), ([70, 3], [5000, 200]), ([2000], [1500]), ([400, 30], [90, 60])], ids=("tokens", "pieces", "tiles", "resident"))
 def test_captured(nq, nk):
     c = Case((8, 1, 128), nq, nk, seed=9)
     ws = c.workspace()
