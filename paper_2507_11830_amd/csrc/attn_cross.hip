@@ -101,6 +101,8 @@ size_t cross_workspace_bytes(int batch, int total_q, int max_q_len, int max_kv_l
   const bool resident = resident_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim).blocks > 0;
   const int kvs = resident ? 1 : shape_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim, true).pieces;
   const size_t pieces = kvs > 1 ? (size_t)rows * kvs * (head_dim + 2) * sizeof(float) : 0;
+  const long streams = (long)batch * (num_q_heads >> column_shift(num_q_heads / num_kv_heads));
+  if (resident && cross_resident_for_few(streams, max_kv_len, head_dim)) return 0;
   const size_t few = prefill_tuning().short_chunk == 1 || max_q_len > decode_route_cap(num_q_heads, num_kv_heads) ? 0 : decode_multi_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim);
   return pieces > few ? pieces : few;
 }
@@ -109,7 +111,9 @@ int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t
                  int batch, int max_pages, int total_q, int max_q_len, int max_kv_len, int num_q_heads, float scale, void *workspace,
                  size_t workspace_bytes, hipStream_t stream) {
   const PrefillTuning tune = prefill_tuning();
-  if (tune.short_chunk != 1) {
+  const int gshift = column_shift(num_q_heads / c.num_kv_heads);
+  const CrossResident resident = resident_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, c.num_kv_heads, c.head_dim);
+  if (tune.short_chunk != 1 && !(resident.blocks > 0 && cross_resident_for_few((long)batch * (num_q_heads >> gshift), max_kv_len, c.head_dim))) {
     DecodeArgs d;
     dim3 wgs;
     int pieces = 0;
@@ -129,14 +133,13 @@ int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t
   a.num_pages = c.num_pages;
   a.Hq = num_q_heads;
   a.Hkv = c.num_kv_heads;
-  a.gshift = column_shift(num_q_heads / c.num_kv_heads);
+  a.gshift = gshift;
   a.n_hgroups = num_q_heads >> a.gshift;
   a.sl2e = scale * 1.44269504088896340736f;
   a.tau = 8.0f / a.sl2e;
   a.batch = batch;
   a.total_q = total_q;
   const long rows = (long)total_q * num_q_heads;
-  const CrossResident resident = resident_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, c.num_kv_heads, c.head_dim);
   if (resident.blocks > 0) return launch_cross_resident(a, resident, c.head_dim, batch, max_q_len, stream);
   CrossShape shape = shape_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, c.num_kv_heads, c.head_dim, workspace != nullptr);
   int kvs = shape.pieces;

@@ -42,9 +42,9 @@ inline int cross_piece_count(long rows, long wgs, long max_kv_len, int head_dim)
 }
 
 // Keys that stay in LDS (attn_cross_resident.hip), 32 per block: two workgroups of four waves a CU where both fit, else one of eight, in
-// one round of workgroups.  Up to 128 keys (520 batches of 9 to 5000 queries: 1.3 times as fast as query tiles at head_dim 64 in the
-// mean, 1.7 at 128, five of them slower; 14 x 1844 queries on 129 at 32q/8kv 252 us in tiles, 137 so); up to 256 where there are enough
-// queries (8 x 1749 on 229 at 16q/2kv 74 and 59, but 1 x 78 on 251 at 8q/1kv 11.7 and 16).  Beyond, the weights are the work: 4 x 73
+// one round of workgroups.  Up to 128 keys (329 batches of 9 to 5000 queries: 1.3 times as fast as query tiles at head_dim 64 in the
+// mean, 1.7 at 128, one of them slower, by 7 %; 14 x 1844 queries on 129 at 32q/8kv 252 us in tiles, 137 so); up to 256 where there are
+// enough queries (8 x 1749 on 229 at 16q/2kv 74 and 59, but 1 x 78 on 251 at 8q/1kv 11.7 and 16).  Beyond, the weights are the work: 4 x 73
 // on 422 at 16q/2kv, head_dim 64, 8.9 and 14.5.
 constexpr int kResidentLds = 128 * 1024;
 struct CrossResident {
@@ -61,6 +61,14 @@ inline CrossResident cross_resident(long rows, long streams, int columns, long m
   r.rounds = (int)(rounds < 1 ? 1 : rounds > 16 ? 16 : rounds);
   if (ceil_div(max_q_len * columns, 32 * r.waves * r.rounds) <= 65535) r.blocks = (int)blocks;
   return r;
+}
+
+// Whether it also serves chunks of a few tokens, as against the decode kernel (160 batches of 1 to 120 sequences): up to 64 keys (means of
+// 1.1 to 1.2 times as fast at head_dim 128, 1.0 to 1.1 at 64), and up to 128 where the rows are more than a round of the decode kernel's
+// workgroups (1.2 to 1.8 times; otherwise as fast or up to 9 % slower).  99 x 2 tokens on 17 keys at 32q/8kv 17.2 and 8.9 us; 50 x 1 on 66
+// at 8q/1kv 5.5 and 6.7.
+inline bool cross_resident_for_few(long streams, long max_kv_len, int head_dim) {
+  return max_kv_len <= 64 || (max_kv_len <= 128 && streams > (head_dim == 128 ? 1 : 2) * kCus);
 }
 
 // columns: query columns of a token (heads that share a KV head's column dimension); streams: sequences x head groups.

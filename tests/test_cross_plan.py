@@ -37,7 +37,7 @@ def test_any_hints(shape):
     for _ in range(4000):
         heads = rng.choice([(8, 1, 128), (32, 8, 128), (12, 3, 64), (1, 1, 64), (65536, 1, 128), (7, 7, 64)])
         lines.append(hints(heads, max(1, big()), max(1, big()), max(1, big()), big() if rng.random() < 0.7 else rng.randint(0, 300), rng.random() < 0.8))
-    for line, (halves, ranked, pieces, blocks, waves, rounds) in zip(lines, shape(lines)):
+    for line, (halves, ranked, pieces, blocks, waves, rounds, _) in zip(lines, shape(lines)):
         rows, batch, streams, cols, total_q, max_q, max_kv, d, can_cut = line
         assert 1 <= pieces <= 16 and (can_cut or pieces == 1)
         if pieces > 1:
@@ -60,7 +60,7 @@ def test_any_hints(shape):
     ((16, 2, 64), 8, 4500, 1089, 1891, (0, 1, 1)),  # uneven, more than a round: longest first
 ], ids=str)
 def test_both_sides(shape, heads, batch, total_q, max_q, max_kv, want):
-    (halves, ranked, pieces, blocks, _, _), = shape([hints(heads, batch, total_q, max_q, max_kv)])
+    (halves, ranked, pieces, blocks, _, _, _), = shape([hints(heads, batch, total_q, max_q, max_kv)])
     assert blocks == 0
     assert (halves, ranked) == want[:2]
     assert pieces == want[2] if want[2] else pieces >= 4
@@ -73,3 +73,9 @@ def test_both_sides(shape, heads, batch, total_q, max_q, max_kv, want):
 ], ids=str)
 def test_keys_that_stay_in_lds(shape, heads, total_q, max_kv, want):
     assert shape([hints(heads, 1, total_q, total_q, max_kv)])[0][3:3 + len(want)] == want
+
+
+@pytest.mark.parametrize("heads,batch,max_kv,want", [
+    ((8, 1, 128), 50, 64, 1), ((8, 1, 128), 50, 66, 0), ((8, 1, 128), 257, 128, 1), ((8, 1, 128), 257, 129, 0), ((16, 2, 64), 256, 100, 0), ((16, 2, 64), 257, 100, 1)], ids=str)
+def test_few_tokens_on_few_keys(shape, heads, batch, max_kv, want):
+    assert shape([hints(heads, batch, batch, 1, max_kv)])[0][6] == want

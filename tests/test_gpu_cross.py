@@ -149,10 +149,12 @@ def test_kernels_behind_it(heads, nq, nk):
     ((71, 1, 64), [9, 40], [1, 2]),
     ((2, 2, 128), [33, 31, 32], [63, 64, 65]),
     ((64, 1, 128), [300, 2], [16, 17]),
+    ((8, 1, 128), [1, 1, 0, 1], [64, 1, 5, 0]),  # few tokens
+    ((32, 8, 128), [3, 1] * 20, [100, 7] * 20),
 ], ids=lambda x: "x".join(map(str, x[:3])))
 def test_keys_that_stay_in_lds(heads, nq, nk):
     c = Case(heads, nq, nk, seed=3)
-    assert c.workspace() is None or max(nq) * heads[0] // heads[1] <= 32
+    assert c.workspace() is None
     c.call(None)
     c.check()
     first = c.out.clone()
