@@ -295,7 +295,11 @@ int sp_norm_rope_append(const sp_cache_desc *cache, const void *q, const void *k
  * Free pages are always taken in ascending order, for the entries of a call's list in their order: results do not
  * depend on timing.
  * Out-of-range rows and page ids are skipped; lengths count as at most max_pages_per_seq * 16.  Calls on one table are
- * ordered by the caller (one stream, or events between them).
+ * ordered by the caller (one stream, or events between them).  With n = 0 nothing is done, and nothing written.
+ *
+ * Tokens are appended to pages that no other row holds: what sp_pages_reserve adds is a row's own, and so is the last page of a
+ * forked row that is not full.  Only sp_pages_release with keep_lens can leave a last page that is shared and no longer full; the
+ * row that goes on from there is then forked once more (the fork gets a page of its own for it), and itself released.
  */
 typedef struct sp_page_table {
   int32_t *ref_counts;  /* device, int32 [num_pages]                                            */

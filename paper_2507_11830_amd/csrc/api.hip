@@ -4,6 +4,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <exception>
 #include <vector>
 
 #include "sp_common.h"
@@ -215,7 +216,7 @@ int sp_norm_rope_append(const sp_cache_desc *cache, const void *q, const void *k
     return fail(SP_ERR_BAD_SHAPE, "strides q %lld k %lld v %lld: tokens must not overlap", (long long)q_stride, (long long)k_stride, (long long)v_stride);
   if (num_q_heads > 0) {
     // a lane group writes a row after it has read the same row, and nothing else
-    const long last = total_new_tokens - 1L, out_bytes = 2 * total_new_tokens * q_row;
+    const long last = total_new_tokens - 1L, out_bytes = 2L * total_new_tokens * q_row;
     const bool in_place = q_out == q && (q_stride == q_row || total_new_tokens == 1);
     if ((!in_place && !apart(q_out, out_bytes, q, 2 * (last * q_stride + q_row))) ||
         (kv && (!apart(q_out, out_bytes, k, 2 * (last * k_stride + kv_row)) || !apart(q_out, out_bytes, v, 2 * (last * v_stride + kv_row)))))
@@ -297,9 +298,8 @@ int sp_pages_copy(const sp_cache_desc *caches, int32_t num_caches, const int32_t
 
 size_t sp_pages_workspace_size(int32_t num_pages, int32_t n) { return num_pages <= 0 || n < 0 ? 0 : pages_workspace_bytes(num_pages, n); }
 
-int sp_debug_validate_pages(const sp_page_table *table) {
-  if (int rc = check_table(table)) return rc;
-  std::vector<int32_t> refs(table->num_pages), lens(table->num_rows), entries((size_t)table->num_rows * table->max_pages_per_seq),
+static int validate_pages(const sp_page_table *table) {
+  std::vector<int32_t> entries((size_t)table->num_rows * table->max_pages_per_seq), refs(table->num_pages), lens(table->num_rows),
       held(table->num_pages, 0);
   hipError_t e = hipMemcpy(refs.data(), table->ref_counts, refs.size() * 4, hipMemcpyDeviceToHost);
   if (e == hipSuccess && !lens.empty()) e = hipMemcpy(lens.data(), table->seq_lens, lens.size() * 4, hipMemcpyDeviceToHost);
@@ -318,6 +318,15 @@ int sp_debug_validate_pages(const sp_page_table *table) {
   for (int p = 0; p < table->num_pages; ++p)
     if (held[p] != refs[p]) return fail(SP_ERR_BAD_SHAPE, "ref_counts[%d]=%d, held by %d entries", p, refs[p], held[p]);
   return SP_OK;
+}
+
+int sp_debug_validate_pages(const sp_page_table *table) {
+  if (int rc = check_table(table)) return rc;
+  try {
+    return validate_pages(table);
+  } catch (const std::exception &) {  // no exception crosses the ABI
+    return fail(SP_ERR_UNSUPPORTED, "sp_debug_validate_pages: no host memory for %d rows of %d pages", table->num_rows, table->max_pages_per_seq);
+  }
 }
 
 static int ulysses_common(bool pack, const void *src, void *dst, int32_t tokens, int32_t num_heads,

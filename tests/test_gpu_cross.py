@@ -232,10 +232,34 @@ def test_sub_ranges_and_padded_buffers():
     sp.sp_attn_cross(c.cache, c.q, c.out, c.cu[1:4], c.lens[1:3], c.table[1:3], 300, 900, c.scale, workspace=c.workspace())
     c.check([1, 2])
     assert torch.isnan(c.out[:5]).all() and torch.isnan(c.out[307:]).all()
+    short = Case((8, 1, 128), [5, 300, 2, 64], [100, 90, 0, 40], seed=17)
+    sp.sp_attn_cross(short.cache, short.q, short.out, short.cu[1:4], short.lens[1:3], short.table[1:3], 300, 90, short.scale)
+    short.check([1, 2])
+    assert torch.isnan(short.out[:5]).all() and torch.isnan(short.out[307:]).all()
     few = Case((8, 1, 128), [4, 3, 1, 2], [100, 900, 0, 400], seed=8)
     sp.sp_attn_cross(few.cache, few.q, few.out, few.cu[1:4], few.lens[1:3], few.table[1:3], 4, 900, few.scale, workspace=few.workspace())
     few.check([1, 2])
     assert torch.isnan(few.out[:4]).all() and torch.isnan(few.out[8:]).all()
+
+
+@pytest.mark.parametrize("most", [20, 128, 300])
+def test_more_sequences_than_a_grid_dimension(most):
+    """70000 sequences of one query on the same pages, of which each sees another number of states."""
+    batch, heads, d = 70000, 2, 64
+    c = Case((heads, 1, d), [batch], [most], seed=10, poison=False)
+    lens = torch.randint(0, most + 1, (batch,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(10))
+    lens[:3] = torch.tensor([0, most, 1])
+    table = c.table.expand(batch, -1).contiguous()
+    ws = sp.sp_attn_cross_workspace_size(batch, batch, 1, most, heads, 1, d)
+    sp.sp_attn_cross(c.cache, c.q, c.out, torch.arange(batch + 1, dtype=torch.int32, device="cuda"), lens.int(), table, 1, most, c.scale,
+                     workspace=torch.empty(ws, dtype=torch.uint8, device="cuda") if ws else None)
+    pos = torch.arange(most, device="cuda")
+    k, v = (p[c.table[0].long()[pos // 16], 0, pos % 16].double() for p in (c.cache.k_pages, c.cache.v_pages))
+    w = (c.q.double().view(-1, d) @ k.t().contiguous()).view(batch, heads, most) * c.scale
+    w = torch.softmax(w.masked_fill(pos[None, None] >= lens[:, None, None], -1e300), -1) * (lens > 0)[:, None, None]
+    w = w.view(-1, most)
+    got, want, size = c.out.double().view(-1, d), w @ v, w @ v.abs()
+    assert ((got - want).abs() <= 2.0**-8 * want.abs() + (2.0**-13 + (2.0**-8 if most > 256 else 0)) * size).all()  # as in Case.check
 
 
 @pytest.mark.parametrize("nq,nk", [([1] * 8, [900] * 8), ([70, 3], [5000, 200]), ([2000], [1500]), ([400, 30], [90, 60])], ids=("tokens", "pieces", "tiles", "resident"))

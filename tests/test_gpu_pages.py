@@ -384,6 +384,30 @@ def test_a_run_of_them_together():
     attend()
 
 
+@pytest.mark.parametrize("pad", (0, 70), ids=("short-lists", "long-lists"))
+def test_cut_back_into_a_shared_page(pad):
+    """A fork that keeps 20 of its parent's 48 tokens goes on in a row of its own: the parent's pages stay as they are."""
+    b = Both(4, 4, 12, pad)
+    cache = make_caches(1, 12, 2, 64)[0]
+    b.reserve([0], [48])
+    b.fork([0], [1])
+    b.release([1], [20])
+    assert b.m.refs[b.m.table[1, 1]] == 2  # shared, and not full
+    bits = cache.k_pages.view(torch.int16)
+    before = bits.clone()
+    lists = b.fork([1], [2])
+    sp.sp_pages_copy(cache, *lists[:2], rows=lists[2])
+    b.release([1])
+    b.reserve([2], [30])
+    own = b.m.table[2, 1]
+    assert b.m.refs[own] == 1 and torch.equal(bits[own, :, :4], before[b.m.table[0, 1], :, :4])
+    new = torch.ones(10, 2, 64, dtype=torch.bfloat16, device="cuda")
+    sp.sp_norm_rope_append(cache, None, new, new, None, dev([0, 10]), dev([20]), b.t.block_table[2:3].contiguous())
+    assert (cache.k_pages[own, :, 4:14] == 1).all()
+    for page in b.m.table[0, :3]:
+        assert torch.equal(bits[page], before[page])
+
+
 def test_captured():
     """A step that drops, forks, copies and grows, as a graph: every replay against the eager calls on the same table."""
     b = Both(20, 10, 300)

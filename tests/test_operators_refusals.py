@@ -261,3 +261,8 @@ def test_marshalling_refuses(seen):
         with pytest.raises(ValueError):
             sp.sp_pages_compact(t, *args, None, stream=0)
     assert not seen
+
+
+def test_no_exception_leaves_the_table_check():
+    assert sp.lib().sp_debug_validate_pages(ctypes.byref(table(num_rows=2**31 - 1, max_pages_per_seq=2**31 - 1))) == UNSUPPORTED
+    assert sp.lib().sp_debug_validate_pages(None) == NULL and sp.lib().sp_debug_validate_pages(ctypes.byref(table(num_pages=0))) == SHAPE
