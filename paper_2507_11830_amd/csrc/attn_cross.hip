@@ -13,8 +13,8 @@
 //     1 to 200 such chunks on 20 to 8000 keys: 22 % faster than query tiles in the mean).  With two column tiles, as in the causal calls,
 //     it took 13 % longer than query tiles in pieces (75 batches);
 //   - few keys, up to 256: they stay in LDS while a workgroup goes through many queries (attn_cross_resident.hip);
-//   - otherwise query tiles of 256 columns (128 at head_dim 64, several workgroups a CU), or of 128 columns whose two wave groups take
-//     alternate key tiles, and where even these leave most CUs idle, in pieces of the key range.
+//   - otherwise query tiles of 128 columns in several workgroups a CU, or of 256 (head_dim 128, long key ranges), or of 128 columns
+//     whose two wave groups take alternate key tiles, and where even these leave most CUs idle, in pieces of the key range.
 #include "decode_stream.h"
 #include "prefill_solo.h"
 #include "cross_plan.h"
@@ -59,13 +59,14 @@ static int launch_cross_stream(const DecodeArgs &a, dim3 wgs, int max_pieces, hi
 
 // ---- longer chunks
 template <int D>
-static int launch_cross_d(const CrossArgs &a, bool split, int batch, int max_q_len, hipStream_t stream) {
+static int launch_cross_d(const CrossArgs &a, const CrossShape &shape, int batch, int max_q_len, hipStream_t stream) {
   constexpr size_t smem = kPrefillSmem<D>;
-  static bool set[3] = {false, false, false};
+  static bool set[4] = {false, false, false, false};
   if (a.kv_splits > 1) return launch_cfg(prefill_kernel<D, KVT, PFD, true, true, 0, CrossArgs>, &set[0], 2 * smem, 128, a, batch, max_q_len, stream);
-  if (split) return launch_cfg(prefill_kernel<D, KVT, PFD, true, false, 0, CrossArgs>, &set[1], 2 * smem, 128, a, batch, max_q_len, stream);
-  if constexpr (D == 64) return launch_cfg(solo_prefill_kernel<CrossArgs>, &set[2], kSoloSmem, kSoloCols, a, batch, max_q_len, stream, kSoloThreads, kSoloLayers);
-  else return launch_cfg(prefill_kernel<D, KVT, PFD, false, false, 0, CrossArgs>, &set[2], smem, 256, a, batch, max_q_len, stream);
+  if (shape.halves) return launch_cfg(prefill_kernel<D, KVT, PFD, true, false, 0, CrossArgs>, &set[1], 2 * smem, 128, a, batch, max_q_len, stream);
+  if (D == 64 || shape.solo) return launch_cfg(solo_prefill_kernel<CrossArgs, D>, &set[2], kSoloSmemOf<D>, kSoloCols, a, batch, max_q_len, stream, kSoloThreads, kSoloLayers);
+  if constexpr (D == 128) return launch_cfg(prefill_kernel<D, KVT, PFD, false, false, 0, CrossArgs>, &set[3], smem, 256, a, batch, max_q_len, stream);
+  return SP_OK;
 }
 
 static int column_shift(int group) {  // log2 of the heads that share the column dimension
@@ -83,7 +84,10 @@ static CrossShape shape_of(int batch, int total_q, int max_q_len, int max_kv_len
   CrossShape s = cross_shape(rows, batch, (long)batch * (num_q_heads >> gshift), 1 << gshift, total_q, max_q_len, max_kv_len, head_dim,
                              can_cut && tune.split == 0);
   if (tune.kv_splits > 0 && can_cut) s.pieces = tune.kv_splits < kv_split_cap(rows) ? tune.kv_splits : kv_split_cap(rows);
-  if (tune.split > 0) s.halves = tune.split == 2;
+  if (tune.split > 0) {
+    s.halves = tune.split == 2;
+    s.solo = false;
+  }
   if (tune.order > 0) s.ranked = tune.order == 2;
   s.ranked = s.ranked && batch <= 64 * kRankSlots;
   return s;
@@ -154,8 +158,7 @@ int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t
   a.ranked = shape.ranked;
   a.rank_shift = 6;
   while (a.rank_shift < 24 && (((long)max_kv_len + max_q_len) >> a.rank_shift) > 63) ++a.rank_shift;
-  const bool split = kvs > 1 || shape.halves;
-  const int rc = c.head_dim == 128 ? launch_cross_d<128>(a, split, batch, max_q_len, stream) : launch_cross_d<64>(a, split, batch, max_q_len, stream);
+  const int rc = c.head_dim == 128 ? launch_cross_d<128>(a, shape, batch, max_q_len, stream) : launch_cross_d<64>(a, shape, batch, max_q_len, stream);
   if (rc != SP_OK || kvs == 1) return rc;
   return launch_combine(a.part_o, a.part_ml, out, rows, kvs, c.head_dim, stream, cu_q, batch, num_q_heads);
 }

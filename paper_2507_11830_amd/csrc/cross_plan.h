@@ -4,7 +4,7 @@
 //
 // Times are estimated in us from constants that leave the least behind on 960 batches drawn at random (eight head shards, 1 to 24
 // sequences, up to 1600 workgroups of 128 columns, 20 to 8192 keys; equal lengths, unequal ones of both sides, unequal keys only;
-// all forms timed): 2.3 % over the best form of each batch, where the causal rules leave 7 %.  Both sides of it: 1 x 1137
+// all forms but solo workgroups timed): 2.3 % over the best form of each batch, where the causal rules leave 7 %.  Both sides of it: 1 x 1137
 // queries on 4580 keys at 32q/4kv in halves 112 us (a second round of workgroups for the last tenth), whole tiles 88; 2 x 206 on 2284 at
 // 16q/2kv 28 and 44; 12 x 17..600 on 65..2500 at 12q/3kv, head_dim 64, 27 and 38.
 #pragma once
@@ -16,6 +16,7 @@ constexpr int kCus = 256;
 
 struct CrossShape {
   bool halves;  // 128 columns, whose keys two wave groups share; else whole tiles of 256 (head_dim 64: 128, three workgroups a CU)
+  bool solo;    // head_dim 128: 128 columns, two workgroups a CU
   bool ranked;  // workgroups take the longest items first; else in (tile, sequence) order
   int pieces;   // of the key ranges (halves only)
 };
@@ -83,6 +84,7 @@ inline CrossShape cross_shape(long rows, int batch, long streams, int columns, l
   // 32q/4kv 28.5 and 39.6).
   auto rank = [&](int cols) { return batch >= 2 && (double)streams * ceil_div(max_q_len * columns, cols) > kCus && (uneven ? tiles >= 2 : max_q_len != max_kv_len && tiles >= 30); };
   CrossShape s;
+  s.solo = false;
   s.pieces = can_cut ? cross_piece_count(rows, wgs, max_kv_len, head_dim) : 1;
   const bool rank_halves = rank(128), rank_whole = rank(head_dim == 128 ? 256 : 128);
   if (s.pieces > 1) {
@@ -90,10 +92,16 @@ inline CrossShape cross_shape(long rows, int batch, long streams, int columns, l
     s.ranked = rank_halves;
     return s;
   }
+  // Workgroups that find work: of even batches as many as the longest chunk has (8 x 550 queries on 1328 keys at 12q/2kv are 288 whole tiles,
+  // two rounds: 70 us, halves 50).
+  auto items = [&](int cols) {
+    const double all = (double)streams * ceil_div(max_q_len * columns, cols);
+    return uneven ? found * 128.0 / cols : all < 1e15 ? all : 1e15;
+  };
   // A tile of an item: 0.55 us in halves, 1 whole; at head_dim 64 0.9, or 0.42 times the workgroups on its CU.  Starts, merges and
   // stores: 10 us a round in halves, 9 whole.  Uneven batches: the mean item at 0.4 of the longest, and half of that (all of it by
   // order) for the end.
-  const double n = (double)found;
+  const double n = items(128);
   auto span = [&](double items, double t, double start, bool ranked) {
     if (!uneven) return (double)(long)((items + kCus - 1) / kCus) * (t + start);
     const double even = items * (0.4 * t + start) / kCus + (ranked ? 0.5 : 1.0) * t;
@@ -101,17 +109,38 @@ inline CrossShape cross_shape(long rows, int batch, long streams, int columns, l
   };
   double whole;
   if (head_dim == 128) {
-    whole = span(n / 2, 1.0 * tiles, 9, rank_whole);
+    whole = span(items(256), 1.0 * tiles, 9, rank_whole);
   } else if (uneven) {
     const double even = n / kCus * 0.4 * 0.42 * tiles + 0.21 * tiles;
     whole = 9 + (even > 0.9 * tiles ? even : 0.9 * tiles);
   } else {
-    const long full = found / (3 * kCus), left = ceil_div(found % (3 * kCus), kCus);  // rounds of three workgroups a CU, and the last
+    const long full = (long)n / (3 * kCus), left = ceil_div((long)n % (3 * kCus), kCus);  // rounds of three workgroups a CU, and the last
     whole = full * (3 * 0.42 * tiles + 9);
     if (left > 0) whole += (0.42 * left > 0.9 ? 0.42 * left : 0.9) * tiles + 9;
   }
-  s.halves = span(n, 0.55 * tiles, 10, rank_halves) <= whole;
+  const double halves = span(n, 0.55 * tiles, 10, rank_halves);
+  s.halves = halves <= whole;
   s.ranked = s.halves ? rank_halves : rank_whole;
+  if (head_dim == 64 || max_kv_len <= 256 || n <= kCus) return s;
+  // Two workgroups of 128 columns on a CU, whose starts and stores are behind each other's multiplications: a tile takes 0.62 us per workgroup
+  // there, one alone 0.8; starts 4 us a round.  Where every workgroup of 128 columns has a CU to itself the halves are faster (500 batches: by
+  // 2 to 25 %, the more keys the more).  On more tiles than about 32 whole tiles, which load every key once per 256 columns,
+  // are as fast or faster.  873 batches on 257 to 6000 keys: 2 % over the best of all forms, 10 % without this one; 12 x 1212 queries on 272
+  // keys at 32q/4kv 151 -> 107 us, 7 x 313 on 529 41.7 -> 31.5; but 6 x 714 on 2014 at 8q/1kv 45.6 and 51.9.
+  const long full = (long)n / (2 * kCus), left = ceil_div((long)n % (2 * kCus), kCus);
+  double solo;
+  if (uneven) {
+    const double even = n / kCus * (0.4 * 0.62 * tiles + 3) + 0.5 * 0.8 * tiles, longest = 0.8 * tiles + 4;
+    solo = even > longest ? even : longest;
+  } else {
+    solo = full * (2 * 0.62 * tiles + 4);
+    if (left > 0) solo += (0.62 * left > 0.8 ? 0.62 * left : 0.8) * tiles + 4;
+  }
+  if (solo < (halves < whole ? halves : whole)) {
+    s.solo = true;
+    s.halves = false;
+    s.ranked = rank_halves;
+  }
   return s;
 }
 

@@ -20,6 +20,10 @@
 // cycles; 797 -> 834 us on 2 x 16k tokens), with 64-key blocks (1950 cycles, 773 us); at head_dim 128, where two such waves share a SIMD, 2250
 // cycles instead of 2380, but twice the tile loads: 1677 -> 1849 us on 1 x 32768 tokens.
 //
+// At head_dim 128 (sp_attn_cross on a few hundred to two thousand keys) two such workgroups share a CU: what it gains over one
+// workgroup of 256 columns is not the loop but its start and end, 9 us of memory round trips, queries and outputs, which the other
+// workgroup's multiplications cover (cross_plan.h: 15 % faster on 257 to 1024 keys, even at 2000).
+//
 // LDS: K[3] and V[2] tile slots in the swizzled layout of SwzTile.  In the period of tile t the waves read K(t) and V(t-1), and
 // the loads of K(t+2) and V(t) are issued into the slots last read in period t-1; they have landed when the period ends.  K is
 // one tile ahead of its use, so that the first operands of period t+1 are read before the barrier that opens it.
@@ -30,11 +34,13 @@ namespace sp {
 
 constexpr int kSoloThreads = 256, kSoloCols = 128, kSoloKSlots = 3, kSoloVSlots = 2;
 constexpr int kSoloLayers = 2;  // half as many columns as the two-group kernel: twice as many query tiles, for the same longest chunk
-constexpr size_t kSoloSmem = (kSoloKSlots + kSoloVSlots) * (size_t)KVT * 64 * 2;
+template <int D>
+constexpr size_t kSoloSmemOf = (kSoloKSlots + kSoloVSlots) * (size_t)KVT * D * 2;
+constexpr size_t kSoloSmem = kSoloSmemOf<64>;
+static_assert(2 * kSoloSmemOf<128> <= 160 * 1024, "two workgroups a CU");
 
-template <typename Args>
-__global__ __launch_bounds__(kSoloThreads, 3) void solo_prefill_kernel(Args a) {
-  constexpr int D = 64;
+template <typename Args, int D = 64>
+__global__ __launch_bounds__(kSoloThreads, D == 64 ? 3 : 2) void solo_prefill_kernel(Args a) {
   using G = TileGeom<D>;
   using Z = SwzTile<D>;
   using std::integral_constant;
@@ -163,7 +169,6 @@ __global__ __launch_bounds__(kSoloThreads, 3) void solo_prefill_kernel(Args a) {
     else n = min(max(__builtin_amdgcn_readfirstlane(pg), 0), a.num_pages - 1);
     return (size_t)(unsigned)n * page_bytes;
   };
-  static_assert(NIW == 2, "two instructions per page");
   const unsigned wave_dst = (unsigned)(w * (NIW * 1024));
   // Every load of this wave has landed; then all waves'.  Not __syncthreads: that would also wait for the operands of the next
   // period that are on their way from LDS (their slot is not written before the period after).  The clobber keeps the
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(kSoloThreads, 3) void solo_prefill_kernel(Args a) {
     auto block = [&](auto bc, auto whatc, int base, auto emit, auto first_of_next) __attribute__((always_inline)) {
       constexpr int B = decltype(bc)::value, I0 = decltype(whatc)::value == 3 ? 0 : NK, N = NOP - I0;
       constexpr int NS = 16, SPO = NS / N;        // scores of a lane, and behind each multiplication
-      static_assert(NS % N == 0 && SPO % 2 == 0, "scores go in pairs");
+      static_assert(NS % N == 0 && (SPO == 1 || SPO % 2 == 0), "scores become weights in pairs");
       mask(base, sc[1 - B]);
       const float msc = m_used * a.sl2e;
       float ls[2] = {0.f, 0.f}, x[NS];
@@ -370,8 +375,8 @@ __global__ __launch_bounds__(kSoloThreads, 3) void solo_prefill_kernel(Args a) {
         }
 #pragma unroll
         for (int e = 0; e < SPO; e += 2) {
-          const int r = SPO * (i - 2) + e;
-          if (r < 0 || r >= NS) continue;
+          const int r = SPO * (i - 2) + e - (SPO == 1);  // SPO 1: a pair in every second step
+          if (r < 0 || r >= NS || r % 2) continue;
           ls[0] += x[r];
           ls[1] += x[r + 1];
           u[r / 8].h[r / 2 % 4] = __builtin_convertvector((f32x2){x[r], x[r + 1]}, bf16x2);

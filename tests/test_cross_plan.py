@@ -37,7 +37,7 @@ def test_any_hints(shape):
     for _ in range(4000):
         heads = rng.choice([(8, 1, 128), (32, 8, 128), (12, 3, 64), (1, 1, 64), (65536, 1, 128), (7, 7, 64)])
         lines.append(hints(heads, max(1, big()), max(1, big()), max(1, big()), big() if rng.random() < 0.7 else rng.randint(0, 300), rng.random() < 0.8))
-    for line, (halves, ranked, pieces, blocks, waves, rounds, _) in zip(lines, shape(lines)):
+    for line, (halves, ranked, pieces, blocks, waves, rounds, _, solo) in zip(lines, shape(lines)):
         rows, batch, streams, cols, total_q, max_q, max_kv, d, can_cut = line
         assert 1 <= pieces <= 16 and (can_cut or pieces == 1)
         if pieces > 1:
@@ -46,6 +46,8 @@ def test_any_hints(shape):
             assert pieces * max(rows // 128, streams) <= 256  # one round
         if batch == 1:
             assert not ranked
+        if solo:
+            assert d == 128 and pieces == 1 and not halves and max_kv > 256
         if blocks > 0:  # all keys fit LDS, twice on a CU with four waves; the grid holds all columns
             assert 32 * blocks >= max_kv and blocks * 128 * d * (2 if waves == 4 else 1) <= 128 * 1024 and waves in (4, 8) and 1 <= rounds <= 16
             assert max_kv <= 256 and -(-max_q * cols // (32 * waves * rounds)) <= 65535 and streams < 2**31
@@ -60,8 +62,8 @@ def test_any_hints(shape):
     ((16, 2, 64), 8, 4500, 1089, 1891, (0, 1, 1)),  # uneven, more than a round: longest first
 ], ids=str)
 def test_both_sides(shape, heads, batch, total_q, max_q, max_kv, want):
-    (halves, ranked, pieces, blocks, _, _, _), = shape([hints(heads, batch, total_q, max_q, max_kv)])
-    assert blocks == 0
+    (halves, ranked, pieces, blocks, _, _, _, solo), = shape([hints(heads, batch, total_q, max_q, max_kv)])
+    assert blocks == 0 and not solo
     assert (halves, ranked) == want[:2]
     assert pieces == want[2] if want[2] else pieces >= 4
     assert shape([hints(heads, batch, total_q, max_q, max_kv, False)])[0][2] == 1
@@ -79,3 +81,12 @@ def test_keys_that_stay_in_lds(shape, heads, total_q, max_kv, want):
     ((8, 1, 128), 50, 64, 1), ((8, 1, 128), 50, 66, 0), ((8, 1, 128), 257, 128, 1), ((8, 1, 128), 257, 129, 0), ((16, 2, 64), 256, 100, 0), ((16, 2, 64), 257, 100, 1)], ids=str)
 def test_few_tokens_on_few_keys(shape, heads, batch, max_kv, want):
     assert shape([hints(heads, batch, batch, 1, max_kv)])[0][6] == want
+
+
+@pytest.mark.parametrize("heads,batch,total_q,max_q,max_kv,want", [
+    ((32, 4, 128), 12, 12 * 1212, 1212, 272, (1, 0)), ((32, 4, 128), 7, 7 * 313, 313, 529, (1, 0)), ((16, 2, 128), 6, 6 * 700, 1300, 700, (1, 1)),
+    ((32, 4, 128), 12, 12 * 1212, 1212, 256, (0, 0)), ((8, 1, 128), 6, 6 * 714, 714, 2014, (0, 0)), ((8, 1, 128), 8, 8 * 4096, 4096, 4096, (0, 0)),
+    ((16, 2, 64), 12, 12 * 1212, 1212, 500, (0, 0))], ids=str)
+def test_two_workgroups_a_cu(shape, heads, batch, total_q, max_q, max_kv, want):
+    s = shape([hints(heads, batch, total_q, max_q, max_kv)])[0]
+    assert (s[7], s[1]) == want

@@ -122,6 +122,8 @@ def test_tile_edges(heads, n):
     ((16, 2, 64), [900] * 8, None),  # several workgroups a CU
     ((32, 8, 128), [700, 1200, 30], [333, 2000, 100]),
     ((2, 2, 64), [3000], [3001]),
+    ((12, 2, 128), [700, 500, 800], [300, 1, 449]),
+    ((5, 5, 128), [1100, 1300, 130, 2000, 7], [511, 257, 256, 270, 640]),
     ((12, 3, 64), [1] * 600, None),  # more sequences than shares are dealt for
 ], ids=lambda x: "x".join(map(str, x[:3])) if x else "any")
 def test_kernels_behind_it(heads, nq, nk):
@@ -167,6 +169,27 @@ def test_keys_that_stay_in_lds(heads, nq, nk):
     c.lens += 1000  # and longer: no more than the hint, in memory
     c.call(None)
     assert first.shape == c.out.shape
+
+
+@pytest.mark.parametrize("heads,nq,nk", [
+    ((32, 8, 128), [500] * 6, [257, 700, 64, 0, 321, 258]),  # also sequences of few keys, and of none
+    ((32, 4, 128), [1300, 40, 257, 1], [900, 901, 63, 1]),
+    ((8, 1, 128), [2000, 2500], [640, 512]),
+    ((12, 2, 128), [1700, 500, 800], [300, 1, 449]),
+    ((5, 5, 128), [2100, 1300, 130, 4000, 7], [511, 257, 256, 270, 640]),
+    ((64, 1, 128), [300, 2, 333], [400, 577, 16]),
+], ids=lambda x: "x".join(map(str, x[:3])))
+def test_two_workgroups_a_cu(heads, nq, nk):
+    c = Case(heads, nq, nk, seed=11)
+    c.call(c.workspace())
+    c.check()
+    first = c.out.clone()
+    grids = kernel_launches(lambda: c.call(c.workspace()))
+    assert len(grids) == 1 and grids[0][1][0] == 256
+    assert torch.equal(first.view(torch.int16), c.out.view(torch.int16))
+    big = Case(heads, nq, nk, seed=12, spread=16.0)  # scores far beyond the first tile's maximum
+    big.call(big.workspace())
+    big.check()
 
 
 def test_the_division_of_the_keys_is_taken():
