@@ -252,17 +252,35 @@ __global__ __launch_bounds__(kPageThreads) void pages_take_kernel(PagesArgs p) {
 // Few entries on a small pool: scan, plan and entries in one workgroup, up to four entries a wave, so one launch instead of two.  Of several
 // entries for one child the first is taken, and entries for one row get their room one after the other.
 constexpr int kSmallWaves = 16, kSmallEntries = 64, kSmallPages = kSmallWaves * 1024, kSmallWidth = 1024;
+constexpr int kSmallPer = kSmallPages / (64 * kSmallWaves);  // words of a wave, every kSmallWaves-th: small pools occupy all waves alike
+
+// The counts of this wave's words, and their free pages to s_bits.
+static __device__ __forceinline__ void small_scan(const PagesArgs &p, int lane, int w, int (&refs)[kSmallPer]) {
+#pragma unroll
+  for (int i = 0; i < kSmallPer; ++i) {
+    refs[i] = 0;
+    if (64 * kSmallWaves * i >= p.num_pages) continue;  // uniform
+    refs[i] = p.refs[min(64 * (kSmallWaves * i + w) + lane, p.num_pages - 1)];
+  }
+}
+static __device__ __forceinline__ void small_bits(const PagesArgs &p, int lane, int w, const int (&refs)[kSmallPer], uint64_t *s_bits) {
+  uint64_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < kSmallPer; ++i) {
+    const uint64_t bits = __builtin_amdgcn_ballot_w64(refs[i] <= 0 && 64 * (kSmallWaves * i + w) + lane < p.num_pages);
+    if (lane == i) mine = bits;
+  }
+  if (lane < kSmallPer) s_bits[kSmallWaves * lane + w] = mine;
+}
 
 template <int OP>
 __global__ __launch_bounds__(64 * kSmallWaves) void pages_small_kernel(PagesArgs p) {
-  constexpr int PER = 16;                               // words of a wave
-  constexpr int WORDS = kSmallWaves * PER, LANE = WORDS / 64;
+  constexpr int WORDS = kSmallWaves * kSmallPer, LANE = WORDS / 64;
   __shared__ uint64_t s_bits[WORDS];
   __shared__ int s_a[kSmallEntries], s_b[kSmallEntries], s_size[kSmallEntries], s_first[kSmallEntries + 1];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int refs[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) refs[i] = p.refs[min(1024 * w + 64 * i + lane, p.num_pages - 1)];
+  int refs[kSmallPer];
+  small_scan(p, lane, w, refs);
   if (w == 0) {
     const bool mine = lane < p.n;
     const int a = mine ? p.a[lane] : -1, b = mine ? p.b[lane] : -1;
@@ -286,13 +304,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void pages_small_kernel(PagesArgs
       if (lane == p.n - 1) s_first[p.n] = incl;
     }
   }
-  uint64_t mine = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const uint64_t bits = __builtin_amdgcn_ballot_w64(refs[i] <= 0 && 1024 * w + 64 * i + lane < p.num_pages);
-    if (lane == i) mine = bits;
-  }
-  if (lane < PER) s_bits[w * PER + lane] = mine;
+  small_bits(p, lane, w, refs, s_bits);
   __syncthreads();
   if (w >= p.n) return;
   // every wave by itself: its entries, and the free pages before each of the lane's words
@@ -431,7 +443,7 @@ __global__ __launch_bounds__(kPageThreads) void pages_rank_kernel(PagesArgs p) {
 constexpr int kSmallTable = 16 * 1024;  // entries
 
 __global__ __launch_bounds__(64 * kSmallWaves) void pages_compact_small_kernel(PagesArgs p) {
-  constexpr int PER = 16, WORDS = kSmallWaves * PER, LANE = WORDS / 64;
+  constexpr int PER = kSmallPer, WORDS = kSmallWaves * PER, LANE = WORDS / 64;
   __shared__ uint64_t s_bits[WORDS];
   __shared__ int s_before[WORDS];                      // free pages before a word
   __shared__ int s_refs[kSmallPages / 2];              // of the i-th page that moves: its count,
@@ -439,8 +451,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void pages_compact_small_kernel(P
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int entries = p.num_rows * p.max_pages;  // at most kSmallTable
   int refs[PER], entry[kSmallTable / (64 * kSmallWaves)], len[kSmallTable / (64 * kSmallWaves)];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) refs[i] = p.refs[min(1024 * w + 64 * i + lane, p.num_pages - 1)];
+  small_scan(p, lane, w, refs);
 #pragma unroll
   for (int i = 0; i < kSmallTable / (64 * kSmallWaves); ++i) {
     const int at = 1024 * i + threadIdx.x;
@@ -449,13 +460,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void pages_compact_small_kernel(P
     entry[i] = p.table[min(at, entries - 1)];
     len[i] = p.lens[min(at, entries - 1) / p.max_pages];
   }
-  uint64_t mine = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const uint64_t bits = __builtin_amdgcn_ballot_w64(refs[i] <= 0 && 1024 * w + 64 * i + lane < p.num_pages);
-    if (lane == i) mine = bits;
-  }
-  if (lane < PER) s_bits[w * PER + lane] = mine;
+  small_bits(p, lane, w, refs, s_bits);
   __syncthreads();
   if (w == 0) {
     int c[LANE], count = 0;
@@ -482,7 +487,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void pages_compact_small_kernel(P
   }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int page = 1024 * w + 64 * i + lane;
+    const int page = 64 * (kSmallWaves * i + w) + lane;
     if (page >= p.num_pages || holes == 0) continue;
     if (page < used && is_free(page)) {
       const int r = free_before(page);
@@ -497,7 +502,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void pages_compact_small_kernel(P
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int page = 1024 * w + 64 * i + lane;
+    const int page = 64 * (kSmallWaves * i + w) + lane;
     if (page < p.num_pages) p.new_refs[page] = page >= used ? 0 : is_free(page) ? s_refs[free_before(page)] : refs[i];
   }
 #pragma unroll
@@ -607,7 +612,7 @@ static int launched(const char *what) {
 }
 
 // Scan and take, or both in one launch where one workgroup is quick enough: up to an entry a wave, or rows that are short together.  A
-// pass of release, fork, copy and reserve: 4 forks of a row of 19 pages 24.8 us with two launches each, 18.4 with one; 41 of up to 17
+// pass of release, fork, copy and reserve: 4 forks of a row of 19 pages 24.8 us with two launches each, 16.6 with one; 41 of up to 17
 // 26 and 21; but 52 of 212 pages 27 and 40.
 template <int OP>
 static void launch_take(const PagesArgs &p, hipStream_t stream) {
