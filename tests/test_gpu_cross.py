@@ -259,6 +259,10 @@ def test_sub_ranges_and_padded_buffers():
     sp.sp_attn_cross(short.cache, short.q, short.out, short.cu[1:4], short.lens[1:3], short.table[1:3], 300, 90, short.scale)
     short.check([1, 2])
     assert torch.isnan(short.out[:5]).all() and torch.isnan(short.out[307:]).all()
+    wide = Case((32, 8, 128), [5, 700, 600, 64], [100, 700, 300, 400], seed=18)
+    sp.sp_attn_cross(wide.cache, wide.q, wide.out, wide.cu[1:4], wide.lens[1:3], wide.table[1:3], 700, 700, wide.scale)
+    wide.check([1, 2])
+    assert torch.isnan(wide.out[:5]).all() and torch.isnan(wide.out[1305:]).all()
     few = Case((8, 1, 128), [4, 3, 1, 2], [100, 900, 0, 400], seed=8)
     sp.sp_attn_cross(few.cache, few.q, few.out, few.cu[1:4], few.lens[1:3], few.table[1:3], 4, 900, few.scale, workspace=few.workspace())
     few.check([1, 2])
@@ -285,7 +289,7 @@ def test_more_sequences_than_a_grid_dimension(most):
     assert ((got - want).abs() <= 2.0**-8 * want.abs() + (2.0**-13 + (2.0**-8 if most > 256 else 0)) * size).all()  # as in Case.check
 
 
-@pytest.mark.parametrize("nq,nk", [([1] * 8, [900] * 8), ([70, 3], [5000, 200]), ([2000], [1500]), ([400, 30], [90, 60])], ids=("tokens", "pieces", "tiles", "resident"))
+@pytest.mark.parametrize("nq,nk", [([1] * 8, [900] * 8), ([70, 3], [5000, 200]), ([2000], [1500]), ([400, 30], [90, 60]), ([700] * 6, [500] * 6)], ids=("tokens", "pieces", "tiles", "resident", "two a CU"))
 def test_captured(nq, nk):
     c = Case((8, 1, 128), nq, nk, seed=9)
     ws = c.workspace()
