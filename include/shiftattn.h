@@ -2,7 +2,8 @@
  * shiftattn — C ABI of the Shift Parallelism attention hot path on one MI355X (gfx950).
  *
  * The operation is causal grouped-query attention over ONE GPU's head shard, reading a
- * paged KV cache.  Source: the paper's section "Introducing Shift Parallelism" and Figure 2.
+ * paged KV cache; with it come what stands right before it (norms, rotation, append), attention
+ * without a mask over the same cache, and the bookkeeping of its pages.  Source: the paper's section "Introducing Shift Parallelism" and Figure 2.
  * Two facts stated there shape this interface: switching between the sequence-parallel
  * (Ulysses) mode and the tensor-parallel mode leaves the KV cache where it is whenever the
  * two degrees multiply to the size of the GPU group, and under either mode a GPU attends
@@ -473,6 +474,8 @@ int sp_debug_validate_hints(const int32_t *cu_seqlens, const int32_t *lens, int3
  *   "prefill_short_chunk" 0 (built-in choice: batches of short chunks go to the decode
  *                   kernels when the workspace allows) or 1 (never; always the prefill kernel).
  *                   Changes what sp_attn_prefill_workspace_size returns.
+ * sp_attn_cross follows "prefill_kv_splits", "prefill_split", "prefill_order" and "prefill_short_chunk" too (with any of the first
+ * three set it takes query tiles also where the keys would stay in LDS), and so does sp_attn_cross_workspace_size.
  * Returns SP_OK, SP_ERR_NULL or SP_ERR_UNSUPPORTED (unknown key / value out of range).
  */
 int sp_debug_set_tuning(const char *key, int32_t value);

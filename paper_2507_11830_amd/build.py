@@ -97,8 +97,9 @@ def spill_limit(kern: str) -> int:
     """Scratch instructions that a kernel's loops may hold.  The 256-column prefill kernels (whole query tiles and the form
     that cuts long ones) and the decode kernels: none.  The 128-column prefill forms: the reloads of their rarely taken
     short-row copy; next to the decode role also one reload in every second tile period of the second wave group.  The
-    equal-share decode with fused append and two column tiles at head_dim 128: per row segment, not per block."""
-    if "solo_prefill_kernel" in kern or "cross_" in kern:
+    equal-share decode with fused append and two column tiles at head_dim 128: per row segment, not per block.  Cross
+    attention on few tokens or few keys, the norms with their append and the page calls: none."""
+    if any(name in kern for name in ("solo_prefill_kernel", "cross_", "norm_rope", "pages_")):
         return 0
     if "prefill_kernel" in kern:
         return 0 if re.search(r"ELb0ELb0E", kern) else 9 if "MixedArgs" in kern else 8
