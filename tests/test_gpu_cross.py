@@ -337,3 +337,12 @@ def test_pages_beyond_four_gigabytes():
     sp.sp_pages_copy(cache, dst, src)  # and back over the boundary
     sp.sp_attn_cross(cache, q, outs[1], cu, lens, far, 40, 70, 0.09)
     assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
+    # the other kernels, which the hint for the keys selects
+    many = torch.randn(4500, 8, 128, generator=g, device="cuda").to(torch.bfloat16)
+    chunks = torch.tensor([0, 500, 4500], dtype=torch.int32, device="cuda")
+    for x, ends, longest, most in ((q, cu, 40, 400), (q[:9], torch.tensor([0, 5, 9], dtype=torch.int32, device="cuda"), 5, 400), (many, chunks, 4000, 300), (many, chunks, 4000, 4000)):
+        got = []
+        for table in (far, near):
+            got.append(torch.full_like(x, float("nan")))
+            sp.sp_attn_cross(cache, x, got[-1], ends, lens, table, longest, most, 0.09)
+        assert torch.equal(got[0].view(torch.int16), got[1].view(torch.int16)) and torch.isfinite(got[0]).all()
