@@ -11,7 +11,8 @@
 // What is chosen from the hints (cross_plan.h says when, and what it measured):
 //   - chunks of a few tokens, one column tile of a wave: the decode kernel with equal shares or fixed splits (75 batches of
 //     1 to 200 such chunks on 20 to 8000 keys: 22 % faster than query tiles in the mean).  With two column tiles, as in the causal calls,
-//     it took 13 % longer than query tiles in pieces (75 batches);
+//     it took 13 % longer than query tiles in pieces (75 batches), but with a workgroup for every column tile it is the faster one
+//     up to about a round of workgroups;
 //   - few keys, up to 256: they stay in LDS while a workgroup goes through many queries (attn_cross_resident.hip);
 //   - otherwise query tiles of 128 columns in several workgroups a CU, or of 256 (head_dim 128, long key ranges), or of 128 columns
 //     whose two wave groups take alternate key tiles, and where even these leave most CUs idle, in pieces of the key range.
@@ -21,37 +22,42 @@
 
 namespace sp {
 
-// ---- chunks of a few tokens
-template <int D>
+// ---- chunks of a few tokens, or column tiles of them.  TILES: the tiles of a chunk in neighbouring workgroups.
+template <int D, bool TILES>
 __global__ __launch_bounds__(64 * kWaves, 2) void cross_stream_kernel(DecodeArgs a) {
   extern __shared__ __align__(16) char smem_raw[];
   lds_char *smem = (lds_char *)smem_raw;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (a.row_splits) {  // fixed splits of a.chunk keys
-    const int hg = blockIdx.x, seq = blockIdx.y, split = blockIdx.z;
+    const int tiles = TILES ? (int)gridDim.x / a.n_hgroups : 1, seq = blockIdx.y, split = blockIdx.z;
+    const int hg = TILES ? (int)blockIdx.x / tiles : (int)blockIdx.x, ct = TILES ? (int)blockIdx.x - hg * tiles : 0;
     const int p0 = split * (a.chunk >> 5);
     const int pages = load_pages(a, seq, p0, 0, w, lane);  // in the same round trip as the lengths
     const int tok = a.cu_q[seq], qn = a.cu_q[seq + 1] - tok, L = cross_keys(a, a.ctx_lens[seq]);
-    if (qn <= 0) return;
+    if (qn <= ct * a.q_cap) return;
     const int p1 = min((L + 31) >> 5, p0 + (a.chunk >> 5)), slot = (seq * a.n_hgroups + hg) * a.row_splits + split;
     if (p1 <= p0) {  // no keys: rows of zeros if there is no other split, else an empty partial
-      if (a.row_splits == 1) zero_chunk<D>(a, tok, qn, hg);
-      else if ((int)threadIdx.x < a.cols) *reinterpret_cast<f32x2 *>(a.part_ml + 2 * ((long)slot * a.cols + threadIdx.x)) = (f32x2){-INFINITY, 0.f};
+      const int c = ct * a.q_cap * a.geff + threadIdx.x;
+      if (a.row_splits > 1) {
+        if ((int)threadIdx.x < a.q_cap * a.geff && c < a.cols) *reinterpret_cast<f32x2 *>(a.part_ml + 2 * ((long)slot * a.cols + c)) = (f32x2){-INFINITY, 0.f};
+      } else if (ct == 0) {
+        zero_chunk<D>(a, tok, qn, hg);
+      }
       return;
     }
-    row_segment<D, false, true, 1, true>(a, smem, lane, w, seq, hg, L, L - qn, tok, p0, p1, pages, a.row_splits == 1, slot);
+    row_segment<D, false, true, 1, true>(a, smem, lane, w, seq, hg, L, L - qn, tok, p0, p1, pages, a.row_splits == 1, slot, ct);
     return;
   }
-  decode_share<D, false, true, 1, true>(a, smem, lane, w, blockIdx.x);
+  if constexpr (!TILES) decode_share<D, false, true, 1, true>(a, smem, lane, w, blockIdx.x);
 }
 
-template <int D>
+template <int D, bool TILES>
 static int launch_cross_stream(const DecodeArgs &a, dim3 wgs, int max_pieces, hipStream_t stream) {
   static bool done = false;
   constexpr int smem = kDecodeShareSmem<D, true>;
-  if (int rc = grant_smem((const void *)cross_stream_kernel<D>, &done, smem)) return rc;
-  hipLaunchKernelGGL((cross_stream_kernel<D>), wgs, dim3(64 * kWaves), smem, stream, a);
+  if (int rc = grant_smem((const void *)cross_stream_kernel<D, TILES>, &done, smem)) return rc;
+  hipLaunchKernelGGL((cross_stream_kernel<D, TILES>), wgs, dim3(64 * kWaves), smem, stream, a);
   if (a.row_splits != 1) launch_decode_combine(a, max_pieces, D, stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SP_OK : fail(SP_ERR_HIP, "sp_attn_cross launch: %s", hipGetErrorString(e));
@@ -100,6 +106,12 @@ static CrossResident resident_of(int batch, int total_q, int max_q_len, int max_
   return cross_resident((long)total_q * num_q_heads, (long)batch * (num_q_heads >> gshift), 1 << gshift, max_q_len, max_kv_len, head_dim);
 }
 
+static CrossTiles tiles_of(int batch, int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim, bool can_split) {
+  const int cap = decode_route_cap(num_q_heads, num_kv_heads), group = num_q_heads / num_kv_heads;
+  const int geff = group < 32 ? group : group % 32 == 0 ? 32 : 1;  // heads of a column tile (set_head_groups)
+  return cross_tiles(batch, num_q_heads / geff, cap, max_q_len, max_kv_len, head_dim, can_split);
+}
+
 size_t cross_workspace_bytes(int batch, int total_q, int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim) {
   const long rows = (long)total_q * num_q_heads;
   const bool resident = resident_of(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim).blocks > 0;
@@ -108,7 +120,10 @@ size_t cross_workspace_bytes(int batch, int total_q, int max_q_len, int max_kv_l
   const long streams = (long)batch * (num_q_heads >> column_shift(num_q_heads / num_kv_heads));
   if (resident && cross_resident_for_few(streams, max_kv_len, head_dim)) return 0;
   const size_t few = prefill_tuning().short_chunk == 1 || max_q_len > decode_route_cap(num_q_heads, num_kv_heads) ? 0 : decode_multi_workspace_bytes(batch, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim);
-  return pieces > few ? pieces : few;
+  const CrossTiles t = tiles_of(batch, max_q_len, max_kv_len, num_q_heads, num_kv_heads, head_dim, true);
+  const size_t tiles = resident || prefill_tuning().short_chunk == 1 ? 0 : cross_tiles_bytes(t, batch, num_q_heads, max_q_len, head_dim);
+  const size_t more = pieces > few ? pieces : few;
+  return more > tiles ? more : tiles;
 }
 
 int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens, const int32_t *block_table,
@@ -123,7 +138,16 @@ int launch_cross(const sp_cache_desc &c, const void *q, void *out, const int32_t
     int pieces = 0;
     if (plan_decode_cross(d, c, q, out, cu_q, kv_lens, block_table, batch, max_pages, max_q_len, max_kv_len, num_q_heads, scale, workspace, workspace_bytes,
                           &wgs, &pieces))
-      return c.head_dim == 128 ? launch_cross_stream<128>(d, wgs, pieces, stream) : launch_cross_stream<64>(d, wgs, pieces, stream);
+      return c.head_dim == 128 ? launch_cross_stream<128, false>(d, wgs, pieces, stream) : launch_cross_stream<64, false>(d, wgs, pieces, stream);
+  }
+  if (tune.short_chunk != 1 && max_pages > 0 && resident.blocks == 0) {
+    const CrossTiles t = tiles_of(batch, max_q_len, max_kv_len, num_q_heads, c.num_kv_heads, c.head_dim, workspace != nullptr);
+    if (t.tiles > 0 && workspace_bytes >= cross_tiles_bytes(t, batch, num_q_heads, max_q_len, c.head_dim)) {
+      DecodeArgs d;
+      plan_cross_tiles(d, c, q, out, cu_q, kv_lens, block_table, batch, max_pages, max_q_len, num_q_heads, scale, workspace, t.chunk, t.splits);
+      const dim3 wgs((unsigned)(d.n_hgroups * t.tiles), (unsigned)batch, (unsigned)t.splits);
+      return c.head_dim == 128 ? launch_cross_stream<128, true>(d, wgs, t.splits, stream) : launch_cross_stream<64, true>(d, wgs, t.splits, stream);
+    }
   }
   CrossArgs a = {};
   a.k_pages = (const char *)c.k_pages;

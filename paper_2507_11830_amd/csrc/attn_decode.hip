@@ -807,6 +807,23 @@ bool plan_decode_cross(DecodeArgs &a, const sp_cache_desc &c, const void *q, voi
   return plan_decode_stream(a, batch, max_q_len, 1, max_kv_len, c.head_dim, workspace, workspace_bytes, 0, true, grid, pieces) == 0;
 }
 
+void plan_cross_tiles(DecodeArgs &a, const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens,
+                      const int32_t *block_table, int batch, int max_pages, int max_q_len, int num_q_heads, float scale, void *workspace, int chunk,
+                      int splits) {
+  set_head_groups(a, num_q_heads, c.num_kv_heads);
+  a.route_cap = 0;
+  set_chunk_args(a, c, nullptr, nullptr, q, cu_q, kv_lens, block_table, max_pages, scale);
+  a.out = (char *)out;
+  a.batch = batch;
+  a.hg_per_kv = a.group / a.geff;
+  a.q_max = max_q_len;
+  a.cols = max_q_len * a.geff;
+  a.row_splits = splits;
+  a.chunk = chunk;
+  a.part_o = (float *)workspace;
+  a.part_ml = a.part_o + (size_t)batch * a.n_hgroups * splits * a.cols * c.head_dim;
+}
+
 // Mixed batches (sequences with a few query tokens next to sequences with long chunks, the usual
 // step of a continuous-batching scheduler): the short ones are served by the split kernel, which
 // skips the others, with partials indexed [sequence][cap tokens][head].  cap = the tokens one

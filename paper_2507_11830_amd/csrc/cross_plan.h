@@ -8,6 +8,8 @@
 // queries on 4580 keys at 32q/4kv in halves 112 us (a second round of workgroups for the last tenth), whole tiles 88; 2 x 206 on 2284 at
 // 16q/2kv 28 and 44; 12 x 17..600 on 65..2500 at 12q/3kv, head_dim 64, 27 and 38.
 #pragma once
+#include <stddef.h>
+
 #include "cut_plan.h"
 
 namespace sp {
@@ -70,6 +72,31 @@ inline CrossResident cross_resident(long rows, long streams, int columns, long m
 // at 8q/1kv 5.5 and 6.7.
 inline bool cross_resident_for_few(long streams, long max_kv_len, int head_dim) {
   return max_kv_len <= 64 || (max_kv_len <= 128 && streams > (head_dim == 128 ? 1 : 2) * kCus);
+}
+
+// Chunks of a few column tiles of a wave (q_cap tokens each): every tile in a workgroup of the decode kernel of its own, which reads the
+// keys again but begins in a third of the time that a query tile takes.  Up to 512 keys each in one launch, where the workgroups are
+// one round (240 batches: 1.28 times as fast in the mean, the worst 0.93; 2 x 16 tokens on 278 keys at 32q/8kv 11.4 -> 7.9 us); longer ranges
+// in splits that are merged, for few workgroups and keys (about 170 batches: 1.12 times, six of them more than 5 % slower; 1 x 64 tokens on
+// 2616 at 32q/4kv 14.8 -> 12.0, but 15 x 33 on 516 at 12q/3kv, head_dim 64, 9.5 and 13.4).
+struct CrossTiles {
+  int tiles;  // 0: not taken
+  int splits, chunk;
+};
+inline CrossTiles cross_tiles(int batch, int n_hgroups, int q_cap, long max_q_len, long max_kv_len, int head_dim, bool can_split) {
+  CrossTiles t = {0, 0, 0};
+  const double rows = (double)batch * n_hgroups * ceil_div(max_q_len, q_cap);
+  const int resident = head_dim == 128 ? kCus : 2 * kCus;
+  if (max_kv_len < 1 || max_q_len <= q_cap || rows > resident || (max_kv_len > 512 && (!can_split || rows > (head_dim == 128 ? 64 : 96) || rows * max_kv_len > 131072))) return t;
+  t.chunk = max_kv_len <= 512 ? 512 : 256;
+  while (max_kv_len > 512 && rows * ceil_div(max_kv_len, t.chunk) > resident) t.chunk += 128;  // ends at 768: the product above
+  t.splits = (int)ceil_div(max_kv_len, t.chunk);
+  t.tiles = (int)ceil_div(max_q_len, q_cap);
+  return t;
+}
+// Bytes of its partials.
+inline size_t cross_tiles_bytes(const CrossTiles &t, int batch, int num_q_heads, long max_q_len, int head_dim) {
+  return t.tiles == 0 || t.splits == 1 ? 0 : (size_t)batch * num_q_heads * max_q_len * t.splits * (head_dim + 2) * sizeof(float);
 }
 
 // columns: query columns of a token (heads that share a KV head's column dimension); streams: sequences x head groups.

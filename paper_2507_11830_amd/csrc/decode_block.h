@@ -165,6 +165,10 @@ int plan_decode_stream(DecodeArgs &a, int batch, int max_q, int tiles, int max_l
 bool plan_decode_cross(DecodeArgs &a, const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens,
                       const int32_t *block_table, int batch, int max_pages, int max_q_len, int max_kv_len, int num_q_heads, float scale,
                       void *workspace, size_t workspace_bytes, dim3 *grid, int *pieces);
+// And for chunks of `tiles` column tiles with fixed splits of `chunk` keys; workspace: what cross_tiles_bytes says.
+void plan_cross_tiles(DecodeArgs &a, const sp_cache_desc &c, const void *q, void *out, const int32_t *cu_q, const int32_t *kv_lens,
+                      const int32_t *block_table, int batch, int max_pages, int max_q_len, int num_q_heads, float scale, void *workspace, int chunk,
+                      int splits);
 void launch_decode_combine(const DecodeArgs &a, int max_pieces, int head_dim, hipStream_t stream);
 // Equal shares for the short sequences of a mixed batch (launch_decode_multi with routed = true): arguments, number of
 // shares and of partials per row.  False where they cannot be taken.

@@ -22,10 +22,10 @@ __device__ __forceinline__ int load_pages(const DecodeArgs &a, int seq, int p0, 
 
 // Key blocks [p0, p1) of one row, by the whole workgroup.  pages: load_pages of the segment's first blocks.
 // whole: they are all of the row's, so the result is the output row; otherwise it goes to partial slot `slot`.
-// CROSS: all query tokens see all L keys (with ctx = L - query tokens).
+// CROSS: all query tokens see all L keys (with ctx = L - query tokens).  ct: the chunk's first column tile of these NT.
 template <int D, bool APPEND, bool MQ, int NT, bool CROSS = false>
 __device__ __forceinline__ void row_segment(const DecodeArgs &a, lds_char *smem, int lane, int w, int seq, int hg, int L, int ctx,
-                                            int tok_base, int p0, int p1, int pages, bool whole, int slot) {
+                                            int tok_base, int p0, int p1, int pages, bool whole, int slot, int ct = 0) {
   using G = TileGeom<D>;
   using Z = SwzTile<D>;
   constexpr int ROWB = D * 2;           // bytes of one K or V row
@@ -39,7 +39,7 @@ __device__ __forceinline__ void row_segment(const DecodeArgs &a, lds_char *smem,
   const int head0 = hg * a.geff;
   const int kvh = a.hg_per_kv == 1 ? hg : hg / a.hg_per_kv;
   const bool writer = a.hg_per_kv == 1 || hg == kvh * a.hg_per_kv;  // fused append: one writer per (position, KV head)
-  const float inv_geff = 1.0f / (float)a.geff;                      // (int)((x + 0.5) / geff) is x / geff for the x < 64 it is used on
+  const float inv_geff = 1.0f / (float)a.geff;                      // (int)((x + 0.5) / geff) is x / geff for x < 65536
   const int kv1 = min(L, 32 * p1);
   const int nb = (p1 - p0 + kWaves - 1 - w) / kWaves;             // blocks of this wave, may be 0
   auto base_of = [&](int i) __attribute__((always_inline)) { return 32 * (p0 + kWaves * i + w); };  // first key of its block i
@@ -51,7 +51,7 @@ __device__ __forceinline__ void row_segment(const DecodeArgs &a, lds_char *smem,
   bf16x8 qreg[NT][G::kDSteps];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int t = nt * a.q_cap + t0;  // tile nt holds the tokens nt * q_cap .. (nt + 1) * q_cap - 1
+    const int t = (ct + nt) * a.q_cap + t0;  // tile nt holds the tokens nt * q_cap .. (nt + 1) * q_cap - 1
     col_valid[nt] = MQ ? t0 < a.q_cap && t < qn : col < a.geff;
     lim_col[nt] = MQ ? (col_valid[nt] && !CROSS ? ctx + t + 1 : L) : 0;
     const char *qrow = a.q + ((long)(tok_base + t) * a.Hq + head0 + h_col) * (D * 2);
@@ -243,7 +243,7 @@ __device__ __forceinline__ void row_segment(const DecodeArgs &a, lds_char *smem,
       if (half == 0) *(lds_f32x2 *)(xml + (w * 32 + col) * 2) = (f32x2){lt == 0.f ? -INFINITY : m[nt] * a.sl2e, lt};
     }
     __syncthreads();
-    const int tile_cols = MQ ? min(max(qn - nt * a.q_cap, 0), a.q_cap) * a.geff : a.geff;
+    const int tile_cols = MQ ? min(max(qn - (ct + nt) * a.q_cap, 0), a.q_cap) * a.geff : a.geff;
     for (int i = threadIdx.x; i < tile_cols * (D / 4); i += 64 * kWaves) {
       const int c = i / (D / 4), ch = 4 * (i - c * (D / 4));
       float M = -INFINITY, den = 0.f;
@@ -262,7 +262,7 @@ __device__ __forceinline__ void row_segment(const DecodeArgs &a, lds_char *smem,
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += f * ou[e];
       }
-      const int tc = nt * a.q_cap * a.geff + c;  // token * geff + head
+      const int tc = (ct + nt) * a.q_cap * a.geff + c;  // token * geff + head
       if (whole) {  // at least one key: M is finite
         const int t = MQ ? (int)(((float)tc + 0.5f) * inv_geff) : 0;
         const float inv = 1.0f / den;

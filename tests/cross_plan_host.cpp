@@ -9,6 +9,8 @@ int main() {
   while (scanf("%ld %d %ld %d %ld %ld %ld %d %d", &rows, &batch, &streams, &columns, &total_q, &max_q, &max_kv, &head_dim, &can_cut) == 9) {
     const sp::CrossShape s = sp::cross_shape(rows, batch, streams, columns, total_q, max_q, max_kv, head_dim, can_cut != 0);
     const sp::CrossResident r = sp::cross_resident(rows, streams, columns, max_q, max_kv, head_dim);
-    printf("%d %d %d %d %d %d %d %d\n", s.halves, s.ranked, s.pieces, r.blocks, r.waves, r.rounds, sp::cross_resident_for_few(streams, max_kv, head_dim), s.solo);
+    const sp::CrossTiles t = sp::cross_tiles(batch, (int)(streams / batch), 32 / columns, max_q, max_kv, head_dim, can_cut != 0);
+    printf("%d %d %d %d %d %d %d %d %d %d %d\n", s.halves, s.ranked, s.pieces, r.blocks, r.waves, r.rounds, sp::cross_resident_for_few(streams, max_kv, head_dim), s.solo,
+           t.tiles, t.splits, t.chunk);
   }
 }

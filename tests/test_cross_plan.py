@@ -37,7 +37,7 @@ def test_any_hints(shape):
     for _ in range(4000):
         heads = rng.choice([(8, 1, 128), (32, 8, 128), (12, 3, 64), (1, 1, 64), (65536, 1, 128), (7, 7, 64)])
         lines.append(hints(heads, max(1, big()), max(1, big()), max(1, big()), big() if rng.random() < 0.7 else rng.randint(0, 300), rng.random() < 0.8))
-    for line, (halves, ranked, pieces, blocks, waves, rounds, _, solo) in zip(lines, shape(lines)):
+    for line, (halves, ranked, pieces, blocks, waves, rounds, _, solo, tiles, splits, chunk) in zip(lines, shape(lines)):
         rows, batch, streams, cols, total_q, max_q, max_kv, d, can_cut = line
         assert 1 <= pieces <= 16 and (can_cut or pieces == 1)
         if pieces > 1:
@@ -46,6 +46,9 @@ def test_any_hints(shape):
             assert pieces * max(rows // 128, streams) <= 256  # one round
         if batch == 1:
             assert not ranked
+        if tiles:  # one round, the chunk covered, the keys too
+            assert max_q * cols > 32 and tiles * (32 // cols) >= max_q and streams * tiles * splits <= (256 if d == 128 else 512)
+            assert splits * chunk >= max_kv > (splits - 1) * chunk and chunk <= 1024 and (can_cut or splits == 1)
         if solo:
             assert d == 128 and pieces == 1 and not halves and max_kv > 256
         if blocks > 0:  # all keys fit LDS, twice on a CU with four waves; the grid holds all columns
@@ -62,7 +65,7 @@ def test_any_hints(shape):
     ((16, 2, 64), 8, 4500, 1089, 1891, (0, 1, 1)),  # uneven, more than a round: longest first
 ], ids=str)
 def test_both_sides(shape, heads, batch, total_q, max_q, max_kv, want):
-    (halves, ranked, pieces, blocks, _, _, _, solo), = shape([hints(heads, batch, total_q, max_q, max_kv)])
+    (halves, ranked, pieces, blocks, _, _, _, solo, *_), = shape([hints(heads, batch, total_q, max_q, max_kv)])
     assert blocks == 0 and not solo
     assert (halves, ranked) == want[:2]
     assert pieces == want[2] if want[2] else pieces >= 4
@@ -90,3 +93,12 @@ def test_few_tokens_on_few_keys(shape, heads, batch, max_kv, want):
 def test_two_workgroups_a_cu(shape, heads, batch, total_q, max_q, max_kv, want):
     s = shape([hints(heads, batch, total_q, max_q, max_kv)])[0]
     assert (s[7], s[1]) == want
+
+
+@pytest.mark.parametrize("heads,batch,max_q,max_kv,want", [
+    ((32, 8, 128), 2, 16, 278, (2, 1)), ((8, 1, 128), 1, 4, 278, (0,)), ((8, 1, 128), 1, 5, 512, (2, 1)), ((8, 1, 128), 1, 5, 513, (2, 3)), ((8, 1, 128), 32, 32, 400, (8, 1)),
+    ((8, 1, 128), 33, 32, 400, (0,)), ((16, 2, 64), 32, 32, 400, (8, 1)), ((16, 2, 64), 33, 32, 400, (0,)), ((8, 1, 128), 8, 32, 2048, (8, 4)), ((8, 1, 128), 8, 32, 2049, (0,)), ((8, 1, 128), 9, 32, 600, (0,)),
+    ((16, 2, 64), 6, 32, 1365, (8, 4)), ((16, 2, 64), 7, 32, 600, (0,)),
+    ((8, 1, 128), 1, 8, 60000, (2, 118)), ((8, 1, 128), 1, 8, 70000, (0,))], ids=str)
+def test_column_tiles(shape, heads, batch, max_q, max_kv, want):
+    assert shape([hints(heads, batch, batch * max_q, max_q, max_kv)])[0][8:8 + len(want)] == want

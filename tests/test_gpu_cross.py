@@ -171,6 +171,37 @@ def test_keys_that_stay_in_lds(heads, nq, nk):
     assert first.shape == c.out.shape
 
 
+@pytest.mark.parametrize("heads,nq,nk,launches", [
+    ((32, 8, 128), [16, 11, 9, 1], [278, 5, 0, 512], 1),
+    ((8, 1, 128), [40, 7, 0, 33], [300, 257, 90, 0], 1),
+    ((8, 1, 128), [33], [2000], 2),
+    ((16, 2, 64), [30, 1, 64], [900, 0, 600], 2),  # a sequence without states
+    ((12, 3, 64), [9, 100, 17], [512, 130, 333], 1),
+    ((7, 1, 64), [5, 41, 4], [700, 20, 650], 2),  # four tokens of seven heads a tile
+    ((71, 1, 64), [40, 2], [200, 130], 1),  # a head a tile
+    ((64, 1, 128), [3, 2], [129, 600], 2),
+    ((5, 5, 128), [90, 33, 32, 31], [400, 1, 129, 64], 1),
+    ((2, 1, 64), [1000], [777], 2),
+    ((8, 1, 128), [8], [60000], 2),
+], ids=lambda x: "x".join(map(str, x[:3])) if isinstance(x, (list, tuple)) else str(x))
+def test_column_tiles(heads, nq, nk, launches):
+    c = Case(heads, nq, nk, seed=13, spread=4.0)
+    ws = c.workspace()
+    assert launches == 1 or ws is not None
+    if ws is not None:
+        ws.fill_(0xFF)
+    c.call(ws)
+    c.check()
+    first = c.out.clone()
+    grids = kernel_launches(lambda: c.call(ws))
+    assert len(grids) == launches and grids[0][1][0] == 256
+    c.out.fill_(float("nan"))
+    c.call(ws)
+    assert torch.equal(first.view(torch.int16), c.out.view(torch.int16))
+    c.call(c.workspace(1) if launches == 2 else None)  # less than it takes: another form
+    c.check()
+
+
 @pytest.mark.parametrize("heads,nq,nk", [
     ((32, 8, 128), [500] * 6, [257, 700, 64, 0, 321, 258]),  # also sequences of few keys, and of none
     ((32, 4, 128), [1300, 40, 257, 1], [900, 901, 63, 1]),
