@@ -281,6 +281,42 @@ def test_no_states_at_all():
         assert (c.out == 0).all()
 
 
+@pytest.mark.parametrize("q,kv", [(1, 3), (3, 1), (20, 1), (1, 20), (50, 50)])
+@pytest.mark.parametrize("heads", [(8, 1, 128), (12, 3, 64)], ids=str)
+def test_hints_larger_than_the_lengths(heads, q, kv):
+    """As of a batch whose buffers are sized for the longest that may come."""
+    for nq, nk in (([3, 1, 0, 4], [40, 0, 9, 200]), ([40, 3, 17], [90, 300, 0]), ([300, 200], [100, 500])):
+        c = Case(heads, nq, nk, seed=14)
+        c.max_q, c.max_kv = c.max_q * q, c.max_kv * kv
+        for ws in (c.workspace(), None):
+            c.out.fill_(float("nan"))
+            c.call(ws)
+            c.check()
+
+
+def test_hints_smaller_than_the_lengths():
+    """Rows that are written are right for the states within the hint and any blocks of those behind it, and nothing else is touched."""
+    for nq, nk, most_q, most_kv in (([9, 30], [100, 300], 5, 300), ([9, 30], [100, 300], 30, 100), ([400, 90], [700, 600], 90, 700), ([33, 40], [900, 2000], 33, 600)):
+        c = Case((8, 1, 128), nq, nk, seed=15)
+        c.q = torch.cat((c.q, c.q[:50]))
+        c.out = torch.full_like(c.q, float("nan"))
+        c.max_q, c.max_kv = most_q, most_kv
+        c.call(c.workspace())
+        for s, (n, m) in enumerate(zip(nq, nk)):
+            a = int(c.cu[s])
+            done = min(n, most_q)
+            got = c.out[a:a + done].double()
+            wants = []
+            for keys in {m, min(m, most_kv), *range(-(-most_kv // 32) * 32, m, 32)}:
+                c.nk[s] = keys
+                wants.append(c.definition(s))
+            ok = torch.zeros(done, dtype=torch.bool, device="cuda")
+            for want, size in wants:
+                ok |= ((got - want[:done]).abs() <= 2.0**-8 * want[:done].abs() + (2.0**-13 + 2.0**-8) * size[:done]).flatten(1).all(1)
+            assert ok.all(), (s, nq, nk)
+        assert torch.isnan(c.out[sum(nq):]).all()
+
+
 def test_sub_ranges_and_padded_buffers():
     c = Case((8, 1, 128), [5, 300, 2, 64], [100, 900, 0, 400], seed=7)
     sp.sp_attn_cross(c.cache, c.q, c.out, c.cu[1:4], c.lens[1:3], c.table[1:3], 300, 900, c.scale, workspace=c.workspace())
