@@ -13,7 +13,7 @@
 //     1 to 200 such chunks on 20 to 8000 keys: 22 % faster than query tiles in the mean).  With two column tiles, as in the causal calls,
 //     it took 13 % longer than query tiles in pieces (75 batches), but with a workgroup for every column tile it is the faster one
 //     up to about a round of workgroups;
-//   - few keys, up to 256: they stay in LDS while a workgroup goes through many queries (attn_cross_resident.hip);
+//   - few keys, up to 256 or 320: they stay in LDS while a workgroup goes through many queries (attn_cross_resident.hip);
 //   - otherwise query tiles of 128 columns in several workgroups a CU, or of 256 (head_dim 128, long key ranges), or of 128 columns
 //     whose two wave groups take alternate key tiles, and where even these leave most CUs idle, in pieces of the key range.
 #include "decode_stream.h"

@@ -51,9 +51,9 @@ inline int cross_piece_count(long rows, long wgs, long max_kv_len, int head_dim)
 //
 // Up to 128 keys (329 batches of 9 to 5000 queries: 1.3 times as fast as query tiles at head_dim 64 in the mean, 1.7 at 128, one of
 // them slower, by 7 %; 14 x 1844 queries on 129 at 32q/8kv 252 us in tiles, 137 so); up to 256 where there are enough queries (8 x 1749 on
-// 229 at 16q/2kv 74 and 59, but 1 x 78 on 251 at 8q/1kv 11.7 and 16).  Beyond, the weights are the work: 4 x 73 on 422 at 16q/2kv,
-// head_dim 64, 8.9 and 14.5.
-constexpr int kResidentLds = 128 * 1024;
+// 229 at 16q/2kv 74 and 59, but 1 x 78 on 251 at 8q/1kv 11.7 and 16), at head_dim 128 and even chunks up to 320 (25 batches on more than 256:
+// 1.13 times as fast as any tiles in the mean; uneven chunks 0.6 to 1.4).  At head_dim 64 the weights are the work there: 0.57 to 1.15.
+constexpr int kResidentLds = 160 * 1024, kResidentPair = 128 * 1024;
 struct CrossResident {
   int blocks;  // 0: not taken
   int waves;
@@ -61,11 +61,11 @@ struct CrossResident {
 };
 inline CrossResident cross_resident(long rows, long streams, int columns, long max_q_len, long max_kv_len, int head_dim) {
   CrossResident r = {0, 0, 0};
-  if (max_kv_len < 1 || max_kv_len > 256 || (max_kv_len > 128 && rows < 48000) || max_q_len > (1 << 24) || streams > 0x7fffffffL) return r;
-  const long blocks = ceil_div(max_kv_len, 32), lds = blocks * 2 * 32 * head_dim * 2;
-  r.waves = 2 * lds <= kResidentLds ? 4 : 8;
-  const long wgs = (r.waves == 4 ? 2 : 1) * kCus, rounds = ceil_div(rows, 32 * r.waves * wgs);
   const bool uneven = 10.0 * rows < 9.0 * streams * columns * max_q_len;
+  if (max_kv_len < 1 || max_kv_len > (head_dim == 128 && !uneven ? 320 : 256) || (max_kv_len > 128 && rows < 48000) || max_q_len > (1 << 24) || streams > 0x7fffffffL) return r;
+  const long blocks = ceil_div(max_kv_len, 32), lds = blocks * 2 * 32 * head_dim * 2;
+  r.waves = 2 * lds <= kResidentPair ? 4 : 8;
+  const long wgs = (r.waves == 4 ? 2 : 1) * kCus, rounds = ceil_div(rows, 32 * r.waves * wgs);
   if (r.waves == 4) r.rounds = (int)(rounds > (uneven ? 3 : 11) ? 3 : rounds);
   else r.rounds = (int)(rounds > (uneven ? 7 : 16) ? (uneven ? 5 : 8) : rounds);
   if (r.rounds < 1) r.rounds = 1;

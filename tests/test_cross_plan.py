@@ -52,8 +52,8 @@ def test_any_hints(shape):
         if solo:
             assert d == 128 and pieces == 1 and not halves and max_kv > 256
         if blocks > 0:  # all keys fit LDS, twice on a CU with four waves; the grid holds all columns
-            assert 32 * blocks >= max_kv and blocks * 128 * d * (2 if waves == 4 else 1) <= 128 * 1024 and waves in (4, 8) and 1 <= rounds <= 64
-            assert max_kv <= 256 and -(-max_q * cols // (32 * waves * rounds)) <= 65535 and streams < 2**31
+            assert 32 * blocks >= max_kv and blocks * 128 * d * (2 if waves == 4 else 1) <= 160 * 1024 and waves in (4, 8) and 1 <= rounds <= 64
+            assert max_kv <= (320 if d == 128 else 256) and -(-max_q * cols // (32 * waves * rounds)) <= 65535 and streams < 2**31
 
 
 @pytest.mark.parametrize("heads,batch,total_q,max_q,max_kv,want", [
@@ -74,7 +74,7 @@ def test_both_sides(shape, heads, batch, total_q, max_q, max_kv, want):
 
 @pytest.mark.parametrize("heads,total_q,max_kv,want", [
     ((8, 1, 128), 57, 10, (1, 4, 1)), ((32, 8, 128), 43303, 18, (1, 4, 3)), ((8, 1, 128), 2**24, 18, (1, 4, 17)), ((8, 1, 128), 78, 128, (4, 4, 1)), ((8, 1, 128), 78, 129, (0,)),
-    ((16, 2, 128), 13992, 229, (8, 8, 4)), ((16, 2, 64), 13992, 256, (8, 4, 4)), ((16, 2, 64), 13992, 257, (0,)), ((16, 2, 64), 100, 0, (0,)),
+    ((16, 2, 128), 13992, 229, (8, 8, 4)), ((16, 2, 64), 13992, 256, (8, 4, 4)), ((16, 2, 64), 13992, 257, (0,)), ((16, 2, 128), 13992, 320, (10, 8, 4)), ((16, 2, 128), 13992, 321, (0,)), ((16, 2, 64), 100, 0, (0,)),
 ], ids=str)
 def test_keys_that_stay_in_lds(shape, heads, total_q, max_kv, want):
     assert shape([hints(heads, 1, total_q, total_q, max_kv)])[0][3:3 + len(want)] == want

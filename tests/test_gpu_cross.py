@@ -145,6 +145,7 @@ def test_kernels_behind_it(heads, nq, nk):
     ((8, 1, 128), [300, 7, 0, 65], [64, 1, 30, 0]),
     ((8, 1, 128), [5000, 10, 40], [128, 97, 0]),
     ((32, 8, 128), [1500, 33, 600], [256, 129, 31]),  # more than 128 keys: one workgroup a CU
+    ((32, 8, 128), [1500, 1400, 1490], [320, 257, 31]),  # of more than 256 keys, and of fewer
     ((12, 3, 64), [200, 500], [32, 33]),
     ((16, 2, 64), [4000, 1], [200, 255]),
     ((7, 1, 64), [50, 3], [33, 100]),
