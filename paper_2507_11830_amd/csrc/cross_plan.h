@@ -47,7 +47,8 @@ inline int cross_piece_count(long rows, long wgs, long max_kv_len, int head_dim)
 // Keys that stay in LDS (attn_cross_resident.hip), 32 per block: two workgroups of four waves a CU where both fit, else one of eight.  One
 // round of them, if that is up to eleven times 32 columns a wave (16 with eight waves); beyond, and where chunks are uneven, shorter ones,
 // whose ends leave less idle (191 even batches of 4 to 40: three instead of up to 16 times 1.1 to 1.18 times as fast from 12 on, 0.85 to 1.03
-// before; 69 uneven ones 1.2 times; but 2 x 65039 queries on 236 at 8q/1kv, 16 times with eight waves, 204 us, five 268).
+// before; 69 uneven ones 1.2 times, with eight waves 102 more 1.05; but 2 x 65039 queries on 236 at 8q/1kv, 16 times with eight waves,
+// 204 us, five 268).
 //
 // Up to 128 keys (329 batches of 9 to 5000 queries: 1.3 times as fast as query tiles at head_dim 64 in the mean, 1.7 at 128, one of
 // them slower, by 7 %; 14 x 1844 queries on 129 at 32q/8kv 252 us in tiles, 137 so); up to 256 where there are enough queries (8 x 1749 on
@@ -66,9 +67,8 @@ inline CrossResident cross_resident(long rows, long streams, int columns, long m
   const long blocks = ceil_div(max_kv_len, 32), lds = blocks * 2 * 32 * head_dim * 2;
   r.waves = 2 * lds <= kResidentPair ? 4 : 8;
   const long wgs = (r.waves == 4 ? 2 : 1) * kCus, rounds = ceil_div(rows, 32 * r.waves * wgs);
-  if (r.waves == 4) r.rounds = (int)(rounds > (uneven ? 3 : 11) ? 3 : rounds);
-  else r.rounds = (int)(rounds > (uneven ? 7 : 16) ? (uneven ? 5 : 8) : rounds);
-  if (r.rounds < 1) r.rounds = 1;
+  const long most = uneven ? 3 : r.waves == 4 ? 11 : 16;
+  r.rounds = (int)(rounds < 1 ? 1 : rounds <= most ? rounds : uneven || r.waves == 4 ? 3 : 8);
   const long least = ceil_div(max_q_len * columns, 32L * r.waves * 65535);  // what the grid holds
   if (r.rounds < least) r.rounds = (int)least;
   r.blocks = (int)blocks;
