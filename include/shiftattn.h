@@ -298,9 +298,13 @@ int sp_norm_rope_append(const sp_cache_desc *cache, const void *q, const void *k
  * Out-of-range rows and page ids are skipped; lengths count as at most max_pages_per_seq * 16.  Calls on one table are
  * ordered by the caller (one stream, or events between them).  With n = 0 nothing is done, and nothing written.
  *
- * Tokens are appended to pages that no other row holds: what sp_pages_reserve adds is a row's own, and so is the last page of a
- * forked row that is not full.  Only sp_pages_release with keep_lens can leave a last page that is shared and no longer full; the
- * row that goes on from there is then forked once more (the fork gets a page of its own for it), and itself released.
+ * Tokens are appended to pages that no other row holds.  What sp_pages_reserve adds is a row's own until a fork shares it, and a
+ * fork shares the row's full pages of written tokens and nothing behind them.  It takes the written tokens from written_lens.  Without
+ * that array all that a row has room for counts as written: a row with room ahead is then cut back to its written tokens
+ * (sp_pages_release with keep_lens) before it is forked, and given its room again afterwards.  Otherwise parent and child share the
+ * pages of tokens to come, and each overwrites the other's.
+ * sp_pages_release with keep_lens can leave a last page that is shared and no longer full; the row that goes on from there is then
+ * forked once more (the fork gets a page of its own for it), and itself released.
  */
 typedef struct sp_page_table {
   int32_t *ref_counts;  /* device, int32 [num_pages]                                            */
@@ -309,6 +313,8 @@ typedef struct sp_page_table {
   int32_t num_pages;
   int32_t num_rows;
   int32_t max_pages_per_seq;
+  const int32_t *written_lens; /* device, int32 [num_rows] tokens of a row whose keys and values are in its pages, or NULL: all
+                                  that it has room for.  The caller's own count: sp_pages_fork reads it, no call writes it */
 } sp_page_table;
 
 /*
@@ -322,11 +328,13 @@ int sp_pages_reserve(const sp_page_table *table, const int32_t *rows, const int3
                      int32_t *shortfall, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * sp_pages_fork — row children[i] becomes a copy of row parents[i]: it holds the same full pages, and if the parent's last page
- * is not full, a page of its own for it, whose rows the caller copies with sp_pages_copy in the cache of every layer:
+ * sp_pages_fork — row children[i] becomes a copy of row parents[i]'s written tokens (written_lens, none beyond seq_lens; seq_lens
+ * itself without it): it holds the same full pages, and if the last of them is not full, a page of its own for it, whose rows the
+ * caller copies with sp_pages_copy in the cache of every layer.  Its seq_lens is that number of tokens; room that the parent has
+ * ahead stays the parent's own:
  *   copy_src, copy_dst, copy_rows  int32 [n] (device, written): rows 0 .. copy_rows[i] - 1 of page copy_src[i] belong into
  *              page copy_dst[i]; -1, -1 and 0 where there is nothing to copy
- * Lengths are those before the call: a parent that is empty then leaves its children empty.  A child is an empty row (seq_lens
+ * Lengths are those before the call: a parent without written tokens then leaves its children empty.  A child is an empty row (seq_lens
  * 0), and named once; entries whose child is not empty are skipped, and of several entries for one child an unspecified one
  * is taken.  All entries or none, shortfall and workspace: as in sp_pages_reserve.
  */

@@ -61,7 +61,7 @@ class sp_rope_desc(ctypes.Structure):
 class sp_page_table(ctypes.Structure):
     _fields_ = [
         ("ref_counts", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("num_pages", ctypes.c_int32),
-        ("num_rows", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("num_rows", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32), ("written_lens", ctypes.c_void_p),
     ]
 
 
@@ -224,25 +224,27 @@ class KVCache:
 
 class PageTable:
     """Which pages every row (sequence) of a block table holds, and how many entries hold a page: int32 cuda tensors
-    block_table [rows, max_pages], seq_lens [rows], ref_counts [num_pages], plus the C descriptor that names them."""
+    block_table [rows, max_pages], seq_lens [rows], ref_counts [num_pages], plus the C descriptor that names them.
+    written_lens: int32 [rows], the caller's count of the tokens that are in a row's pages, where rows have room ahead of them
+    (what sp_pages_fork shares); None: rows are written up to seq_lens."""
 
-    def __init__(self, block_table, seq_lens, ref_counts):
+    def __init__(self, block_table, seq_lens, ref_counts, written_lens=None):
         import torch
 
-        for t in (block_table, seq_lens, ref_counts):
+        for t in (block_table, seq_lens, ref_counts, *(() if written_lens is None else (written_lens,))):
             assert t.is_cuda and t.is_contiguous() and t.dtype == torch.int32
         rows, max_pages = block_table.shape
-        assert seq_lens.shape == (rows,) and ref_counts.dim() == 1
-        self.block_table, self.seq_lens, self.ref_counts = block_table, seq_lens, ref_counts
-        self.desc = sp_page_table(ref_counts.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), ref_counts.shape[0], rows, max_pages)
+        assert seq_lens.shape == (rows,) and ref_counts.dim() == 1 and (written_lens is None or written_lens.shape == (rows,))
+        self.block_table, self.seq_lens, self.ref_counts, self.written_lens = block_table, seq_lens, ref_counts, written_lens
+        self.desc = sp_page_table(ref_counts.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), ref_counts.shape[0], rows, max_pages, _ptr(written_lens))
 
     @classmethod
-    def empty(cls, num_rows: int, max_pages: int, num_pages: int, device="cuda:0"):
+    def empty(cls, num_rows: int, max_pages: int, num_pages: int, device="cuda:0", written_lens=None):
         """No row holds a page."""
         import torch
 
         return cls(torch.full((num_rows, max_pages), -1, dtype=torch.int32, device=device),
-                   torch.zeros(num_rows, dtype=torch.int32, device=device), torch.zeros(num_pages, dtype=torch.int32, device=device))
+                   torch.zeros(num_rows, dtype=torch.int32, device=device), torch.zeros(num_pages, dtype=torch.int32, device=device), written_lens)
 
 
 def sp_version() -> int:
@@ -329,7 +331,8 @@ def sp_pages_reserve(table: PageTable, rows, new_lens, shortfall, workspace, str
 
 
 def sp_pages_fork(table: PageTable, parents, children, copy_src, copy_dst, copy_rows, shortfall, workspace, stream=None) -> None:
-    """All int32 [n], shortfall [1].  The copies that are asked for in copy_* are made by sp_pages_copy."""
+    """All int32 [n], shortfall [1].  The copies that are asked for in copy_* are made by sp_pages_copy.  A parent with room ahead of
+    its written tokens needs table.written_lens, or is released to them before."""
     _check((_native or _calls()).pages_fork(table, parents, children, copy_src, copy_dst, copy_rows, shortfall, workspace, stream))
 
 

@@ -47,6 +47,7 @@ __host__ __device__ __forceinline__ int pages_of(int tokens) { return tokens <= 
 
 struct PagesArgs {
   int32_t *refs, *table, *lens;
+  const int32_t *written;  // or null: rows are written up to their length
   int num_pages, num_rows, max_pages, nseg;
   uint64_t *free_bits;  // [nseg * kSegWords]
   int32_t *seg_free;    // [nseg] free pages of a segment
@@ -54,7 +55,7 @@ struct PagesArgs {
   const int32_t *a, *b;  // rows and new lengths; parents and children
   int n;
   int32_t *plan;   // [n + 1] pages that the entries before take
-  int32_t *sizes;  // [n] fork: the parent's tokens, -1 for a skipped entry; reserve: the row's pages to be, 0 for a skipped entry
+  int32_t *sizes;  // [n] fork: the parent's written tokens, -1 for a skipped entry; reserve: the row's pages to be, 0 for a skipped entry
   int32_t *shortfall, *copy_src, *copy_dst, *copy_rows;
   // compact
   int32_t *new_table, *new_refs, *move_src, *move_dst, *moved;
@@ -66,6 +67,12 @@ static __device__ __forceinline__ int row_tokens(const PagesArgs &p, int row) {
   const long most = (long)p.max_pages * kPage;
   const int len = p.lens[row];
   return len < 0 ? 0 : len > most ? (int)most : len;
+}
+
+// Those of them that a fork takes over.  Pages behind them are the row's own: it is still to append there.
+static __device__ __forceinline__ int forked_tokens(const PagesArgs &p, int row) {
+  const int room = row_tokens(p, row);
+  return p.written ? min(max(p.written[row], 0), room) : room;
 }
 
 enum { kCompact, kReserve, kFork };
@@ -112,7 +119,7 @@ __global__ __launch_bounds__(kPageThreads) void pages_scan_kernel(PagesArgs p) {
         if (a >= 0 && a < p.num_rows) {
           if (OP == kFork) {
             if (b >= 0 && b < p.num_rows && p.lens[b] == 0) {
-              size = row_tokens(p, a);
+              size = forked_tokens(p, a);
               need = size % kPage != 0;
             }
           } else if (pages_of(b) <= p.max_pages) {
@@ -285,7 +292,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void pages_small_kernel(PagesArgs
     const bool mine = lane < p.n;
     const int a = mine ? p.a[lane] : -1, b = mine ? p.b[lane] : -1;
     const bool row = a >= 0 && a < p.num_rows, child = OP == kFork && row && b >= 0 && b < p.num_rows;
-    const int tokens = row ? row_tokens(p, a) : 0, child_len = child ? p.lens[b] : 1;
+    const int tokens = !row ? 0 : OP == kFork ? forked_tokens(p, a) : row_tokens(p, a), child_len = child ? p.lens[b] : 1;
     int size = OP == kFork ? (child && child_len == 0 ? tokens : -1) : (row && pages_of(b) <= p.max_pages ? pages_of(b) : 0);
     int has = pages_of(tokens);
     for (int j = 0; j < p.n - 1; ++j) {  // entries before this one
@@ -586,6 +593,7 @@ static PagesArgs pages_args(const sp_page_table &t, void *workspace, int n) {
   p.refs = t.ref_counts;
   p.table = t.block_table;
   p.lens = t.seq_lens;
+  p.written = t.written_lens;
   p.num_pages = t.num_pages;
   p.num_rows = t.num_rows;
   p.max_pages = t.max_pages_per_seq;

@@ -446,3 +446,109 @@ def test_captured():
         torch.cuda.synchronize()
         for x, y in zip(state, want):
             assert torch.equal(x.view(torch.int16), y.view(torch.int16)) if x.dtype == torch.bfloat16 else torch.equal(x, y)
+
+
+class Ahead(Both):
+    """Rows with room ahead of what is written in them."""
+
+    def __init__(self, rows, width, pages, pad=0):
+        super().__init__(rows, width, pages, pad)
+        self.written = np.zeros(rows, int)
+        self.device = dev(self.written)
+        self.t = sp.PageTable(self.t.block_table, self.t.seq_lens, self.t.ref_counts, self.device)
+
+    def fork(self, parents, children):
+        self.device.copy_(dev(self.written))
+        m, parents, children = self.m, [*parents, *[-1] * self.pad], [*children, *[0] * self.pad]
+        tokens = np.minimum(np.maximum(self.written, 0), m.lens)
+        ok = [p >= 0 and m.lens[c] == 0 for p, c in zip(parents, children)]
+        free, copies = m.free(), []
+        need = sum(bool(o and tokens[p] % 16) for o, p in zip(ok, parents))
+        want = max(need - len(free), 0)
+        for o, p, c in zip(ok, parents, children):
+            copies.append((-1, -1, 0))
+            if not o or want:
+                continue
+            n = tokens[p]
+            for i in range(n // 16):
+                m.table[c, i] = m.table[p, i]
+                m.refs[m.table[p, i]] += 1
+            if n % 16:
+                m.table[c, n // 16] = q = free.pop(0)
+                m.refs[q] = 1
+                copies[-1] = (m.table[p, n // 16], q, n % 16)
+            m.lens[c] = self.written[c] = n
+        lists = [dev([-9] * len(parents)) for _ in range(3)]
+        sp.sp_pages_fork(self.t, dev(parents), dev(children), *lists, self.short, self.ws)
+        assert int(self.short) == want
+        assert [tuple(x) for x in torch.stack(lists, 1).tolist()] == copies
+        self.same()
+        return lists
+
+
+@pytest.mark.parametrize("pad", (0, 70), ids=("short-lists", "long-lists"))
+@pytest.mark.parametrize("pages", (65, 700, 16385))
+def test_forks_of_rows_with_room_ahead(pages, pad):
+    """A page that is still to be written has one holder, whatever is forked in which order."""
+    rng = np.random.default_rng(pages)
+    rows, width = 40, 30
+    b = Ahead(rows, width, pages, pad)
+    for step in range(30):
+        pick = rng.choice(rows, rng.integers(2, 12), replace=False)
+        what = rng.choice(["reserve", "write", "fork", "fork", "release", "cut"])
+        if what == "reserve":
+            b.reserve(pick, rng.integers(1, min(16 * width, 2 * pages), len(pick)))
+        elif what == "write":
+            b.written[pick] += rng.integers(0, b.m.lens[pick] - b.written[pick] + 1)
+        elif what == "fork":
+            k = len(pick) // 2
+            b.fork(rng.choice(pick[:k], 8), rng.choice(np.setdiff1d(np.arange(rows), pick[:k]), 8, replace=False))
+        elif what == "release":
+            b.written[pick] = 0
+            b.release(pick)
+        else:
+            b.release(pick, b.written[pick] + rng.integers(0, 40, len(pick)))
+        for r in range(rows):
+            assert (b.m.refs[b.m.table[r, b.written[r] // 16:pages_of(b.m.lens[r])]] == 1).all()
+
+
+def test_written_lengths_outside_the_room():
+    for pad in (0, 70):
+        b = Ahead(6, 8, 40, pad)
+        b.reserve([0, 1, 2], [100, 40, 16])
+        b.written[:3] = [2**31 - 1, -5, 16]  # no more than the room, and none
+        b.fork([0, 1, 2], [3, 4, 5])
+        assert b.m.lens.tolist() == [100, 40, 16, 100, 0, 16]
+
+
+@pytest.mark.parametrize("cut", (False, True), ids=("written-lens", "cut-back-first"))
+@pytest.mark.parametrize("pad", (0, 70), ids=("short-lists", "long-lists"))
+def test_parent_and_child_go_on_in_pages_of_their_own(pad, cut):
+    """A row with room for 100 tokens of which 40 are written is forked; both then append, and both keep what they have."""
+    pages, hkv, d = 30, 2, 64
+    b = Both(3, 8, pages, pad) if cut else Ahead(3, 8, pages, pad)
+    cache = make_caches(1, pages, hkv, d)[0]
+    tokens = {0: torch.randn(40, hkv, d, device="cuda").to(torch.bfloat16)}
+
+    def append(row, ctx, x):
+        sp.sp_norm_rope_append(cache, None, x, x, None, dev([0, len(x)]), dev([ctx]), b.t.block_table[row:row + 1].contiguous())
+
+    b.reserve([0], [100])
+    append(0, 0, tokens[0])
+    if cut:
+        b.release([0], [40])
+    else:
+        b.written[0] = 40
+    lists = b.fork([0], [1])
+    sp.sp_pages_copy(cache, lists[0], lists[1], rows=lists[2])
+    tokens[1] = tokens[0]
+    b.reserve([0, 1], [100, 90])
+    for row, n in ((0, 60), (1, 50)):
+        new = torch.randn(n, hkv, d, device="cuda").to(torch.bfloat16)
+        append(row, 40, new)
+        tokens[row] = torch.cat((tokens[row], new))
+    for row in (0, 1):
+        pos = torch.arange(len(tokens[row]), device="cuda")
+        page = b.t.block_table[row].long()[pos // 16]
+        for pool in (cache.k_pages, cache.v_pages):
+            assert torch.equal(pool[page, :, pos % 16], tokens[row])
