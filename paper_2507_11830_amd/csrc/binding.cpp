@@ -85,6 +85,38 @@ bool dims(PyObject *t, int32_t *out, Py_ssize_t n, bool exactly) {  // the first
   return ok;
 }
 
+bool steps_of(PyObject *t, int64_t *out, Py_ssize_t n) {
+  PyObject *s = PyObject_CallMethodNoArgs(t, s_stride);
+  PyObject *fast = s ? PySequence_Fast(s, "stride is not a sequence") : nullptr;
+  Py_XDECREF(s);
+  if (!fast) return false;
+  for (Py_ssize_t i = 0; i < n; ++i) out[i] = i < PySequence_Fast_GET_SIZE(fast) ? PyLong_AsLongLong(PySequence_Fast_GET_ITEM(fast, i)) : 0;
+  Py_DECREF(fast);
+  return !PyErr_Occurred();
+}
+
+// Elements of the width that is read: whole numbers of 4 bytes (torch's own have 8), angles of 4, weights of 2.
+bool sized(PyObject *t, const char *name, long bytes) {
+  PyObject *e = PyObject_CallMethodNoArgs(t, s_element_size);
+  if (!e) return false;
+  const long have = PyLong_AsLong(e);
+  Py_DECREF(e);
+  if (have == bytes) return true;
+  if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "%s: elements of %ld bytes, not %ld", name, bytes, have);
+  return false;
+}
+
+// A list of n elements that follow each other; n -1: any number, which it becomes.
+bool list_of(PyObject *t, const char *name, long bytes, int32_t *n) {
+  int32_t size;
+  int64_t step = 1;
+  if (!dims(t, &size, 1, true) || !sized(t, name, bytes) || (size > 1 && !steps_of(t, &step, 1))) return false;
+  if (step != 1) return PyErr_Format(PyExc_ValueError, "%s: not contiguous", name), false;
+  if (*n >= 0 && size != *n) return PyErr_Format(PyExc_ValueError, "%s: %d entries, not %d", name, (int)size, (int)*n), false;
+  *n = size;
+  return true;
+}
+
 bool bytes_of(PyObject *t, size_t *out) {
   *out = 0;
   if (t == Py_None) return true;
@@ -129,6 +161,15 @@ bool scale_of(PyObject *o, float *out) {
   if (!v) return false;
   *out = (float)PyFloat_AS_DOUBLE(v);
   Py_DECREF(v);
+  return true;
+}
+
+// At least n counters of 32 bits.
+bool counters(PyObject *t, const char *name, size_t n) {
+  size_t bytes;
+  if (t == Py_None) return true;  // the library says whether it takes none
+  if (!sized(t, name, 4) || !bytes_of(t, &bytes)) return false;
+  if (bytes < 4 * n) return PyErr_Format(PyExc_ValueError, "%s: at least %zu entries", name, n), false;
   return true;
 }
 
@@ -283,8 +324,9 @@ PyObject *attn_cross(PyObject *, PyObject *const *a, Py_ssize_t n) {
   size_t ws_bytes;
   if (!count("attn_cross", n, 11, kCross) || !dims(a[5], table, 2, true) || !dims(a[1], q, 2, false) || !bytes_of(a[9], &ws_bytes) || !desc.take(a[0]))
     return nullptr;
+  static const char *const names[] = {"cu_seqlens_q", "kv_lens", "block_table"};
   for (int i = 0; i < 5; ++i)
-    if (!pointer(a[1 + i], p + i)) return nullptr;
+    if ((i >= 2 && a[1 + i] != Py_None && !sized(a[1 + i], names[i - 2], 4)) || !pointer(a[1 + i], p + i)) return nullptr;
   if (!scale_of(a[8], &scale) || !pointer(a[9], &ws) || !stream_of(a[10], &stream) || !int32(a[6], &max_q) || !int32(a[7], &max_kv)) return nullptr;
   return finish([&] {
     return ((decltype(&sp_attn_cross))entries[kCross].fn)(desc.get(), p[0], p[1], (const int32_t *)p[2], (const int32_t *)p[3],
@@ -297,16 +339,8 @@ PyObject *attn_cross(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // of the tensors before it, or -1.
 bool rows_of(PyObject *t, const char *name, int32_t head_dim, int32_t *tokens, int32_t *heads, int64_t *stride) {
   int32_t size[3];
-  if (!dims(t, size, 3, true)) return false;
-  PyObject *s = PyObject_CallMethodNoArgs(t, s_stride);
-  PyObject *fast = s ? PySequence_Fast(s, "stride is not a sequence") : nullptr;
-  Py_XDECREF(s);
-  if (!fast) return false;
-  int64_t step[3] = {0, 0, 0};
-  if (PySequence_Fast_GET_SIZE(fast) == 3)
-    for (int i = 0; i < 3; ++i) step[i] = PyLong_AsLongLong(PySequence_Fast_GET_ITEM(fast, i));
-  Py_DECREF(fast);
-  if (PyErr_Occurred()) return false;
+  int64_t step[3];
+  if (!dims(t, size, 3, true) || !steps_of(t, step, 3)) return false;
   const int64_t row = (int64_t)size[1] * size[2];
   if (size[2] != head_dim || (*tokens >= 0 && size[0] != *tokens) || (size[0] > 0 && (step[2] != 1 || (size[1] > 1 && step[1] != size[2])))) {
     PyErr_Format(PyExc_ValueError, "%s: [tokens][heads][%d] with contiguous heads, as many tokens as the others", name, (int)head_dim);
@@ -326,7 +360,8 @@ PyObject *norm_rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   int64_t strides[3] = {0, 0, 0};
   float eps;
   if (!count("norm_rope_append", n, 15, kNormRope) || !desc.take(a[0])) return nullptr;
-  const int32_t d = desc.get()->head_dim, hkv = desc.get()->num_kv_heads;
+  int32_t d = desc.get()->head_dim;
+  const int32_t hkv = desc.get()->num_kv_heads;
   if (a[7] == Py_None ? !dims(a[6], table, 1, false) : !dims(a[7], table, 2, true)) return nullptr;
   if (a[1] != Py_None) {
     int32_t ho;
@@ -343,17 +378,36 @@ PyObject *norm_rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     PyErr_Format(PyExc_ValueError, "k and v: the cache has %d heads", (int)hkv);
     return nullptr;
   }
+  if (tokens < 0) {
+    PyErr_SetString(PyExc_ValueError, "norm_rope_append: k and v, queries, or both");
+    return nullptr;
+  }
+  static const char *const names[] = {"cu_seqlens_new", "ctx_lens", "block_table", "q_weight", "k_weight"};
+  for (int i = 0; i < 5; ++i)
+    if (a[5 + i] != Py_None && !(i < 3 ? sized(a[5 + i], names[i], 4) : list_of(a[5 + i], names[i], 2, &d))) return nullptr;
+  if (a[11] != Py_None) {
+    int64_t step[2];
+    if (!dims(a[11], angles, 2, true) || !sized(a[11], "cos_sin", 4) || !steps_of(a[11], step, 2)) return nullptr;
+    if ((angles[1] > 1 && step[1] != 1) || (angles[0] > 1 && step[0] != angles[1])) {
+      PyErr_SetString(PyExc_ValueError, "cos_sin: not contiguous");
+      return nullptr;
+    }
+  }
+  if (a[13] != Py_None) {
+    int32_t have = -1;
+    if (!list_of(a[13], "positions", 4, &have)) return nullptr;
+    if (have < tokens) return PyErr_Format(PyExc_ValueError, "positions: %d entries for %d tokens", (int)have, (int)tokens);
+  }
   for (int i = 0; i < 9; ++i)
     if (!pointer(a[1 + i], p + i)) return nullptr;
   if (!scale_of(a[10], &eps) || !pointer(a[11], &cos_sin) || !pointer(a[13], &positions) || !stream_of(a[14], &stream)) return nullptr;
-  if (a[11] != Py_None && !dims(a[11], angles, 2, true)) return nullptr;
   const int interleaved = PyObject_IsTrue(a[12]);
   if (interleaved < 0) return nullptr;
   const sp_rope_desc rope = {(const float *)cos_sin, angles[0], angles[1], interleaved};
   return finish([&] {
     return ((decltype(&sp_norm_rope_append))entries[kNormRope].fn)(
         desc.get(), p[0], p[1], p[2], strides[0], strides[1], strides[2], p[3], p[7], p[8], eps, a[11] == Py_None ? nullptr : &rope,
-        (const int32_t *)positions, (const int32_t *)p[4], (const int32_t *)p[5], (const int32_t *)p[6], table[0], table[1], tokens < 0 ? 0 : tokens, hq,
+        (const int32_t *)positions, (const int32_t *)p[4], (const int32_t *)p[5], (const int32_t *)p[6], table[0], table[1], tokens, hq,
         stream);
   });
 }
@@ -362,12 +416,11 @@ PyObject *norm_rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyObject *pages_reserve(PyObject *, PyObject *const *a, Py_ssize_t n) {
   Desc desc;
   void *p[4], *stream;
-  int32_t entries_n, more;
+  int32_t entries_n = -1;
   size_t ws_bytes;
-  if (!count("pages_reserve", n, 6, kReserve) || !dims(a[1], &entries_n, 1, true) || !dims(a[2], &more, 1, true) || !bytes_of(a[4], &ws_bytes) ||
-      !desc.take_table(a[0]))
+  if (!count("pages_reserve", n, 6, kReserve) || !list_of(a[1], "rows", 4, &entries_n) || !list_of(a[2], "new_lens", 4, &entries_n) ||
+      !counters(a[3], "shortfall", 1) || !bytes_of(a[4], &ws_bytes) || !desc.take_table(a[0]))
     return nullptr;
-  if (more != entries_n) return PyErr_Format(PyExc_ValueError, "rows and new_lens: %d and %d entries", (int)entries_n, (int)more);
   for (int i = 0; i < 4; ++i)
     if (!pointer(a[1 + i], p + i)) return nullptr;
   if (!stream_of(a[5], &stream)) return nullptr;
@@ -381,19 +434,18 @@ PyObject *pages_reserve(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
   Desc desc;
   void *p[7], *stream;
-  int32_t sizes[5];
+  int32_t entries_n = -1;
   size_t ws_bytes;
   if (!count("pages_fork", n, 9, kFork)) return nullptr;
-  for (int i = 0; i < 5; ++i) {
-    if (!dims(a[1 + i], sizes + i, 1, true)) return nullptr;
-    if (sizes[i] != sizes[0]) return PyErr_Format(PyExc_ValueError, "%d parents, and an array of %d entries", (int)sizes[0], (int)sizes[i]);
-  }
-  if (!bytes_of(a[7], &ws_bytes) || !desc.take_table(a[0])) return nullptr;
+  static const char *const names[] = {"parents", "children", "copy_src", "copy_dst", "copy_rows"};
+  for (int i = 0; i < 5; ++i)
+    if (!list_of(a[1 + i], names[i], 4, &entries_n)) return nullptr;
+  if (!counters(a[6], "shortfall", 1) || !bytes_of(a[7], &ws_bytes) || !desc.take_table(a[0])) return nullptr;
   for (int i = 0; i < 7; ++i)
     if (!pointer(a[1 + i], p + i)) return nullptr;
   if (!stream_of(a[8], &stream)) return nullptr;
   return finish([&] {
-    return ((decltype(&sp_pages_fork))entries[kFork].fn)(desc.table(), (const int32_t *)p[0], (const int32_t *)p[1], sizes[0], (int32_t *)p[2],
+    return ((decltype(&sp_pages_fork))entries[kFork].fn)(desc.table(), (const int32_t *)p[0], (const int32_t *)p[1], entries_n, (int32_t *)p[2],
                                                          (int32_t *)p[3], (int32_t *)p[4], (int32_t *)p[5], p[6], ws_bytes, stream);
   });
 }
@@ -402,12 +454,9 @@ PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyObject *pages_release(PyObject *, PyObject *const *a, Py_ssize_t n) {
   Desc desc;
   void *p[2], *stream;
-  int32_t entries_n, more;
-  if (!count("pages_release", n, 4, kRelease) || !dims(a[1], &entries_n, 1, true) || !desc.take_table(a[0])) return nullptr;
-  if (a[2] != Py_None) {
-    if (!dims(a[2], &more, 1, true)) return nullptr;
-    if (more != entries_n) return PyErr_Format(PyExc_ValueError, "rows and keep_lens: %d and %d entries", (int)entries_n, (int)more);
-  }
+  int32_t entries_n = -1;
+  if (!count("pages_release", n, 4, kRelease) || !list_of(a[1], "rows", 4, &entries_n) || !desc.take_table(a[0])) return nullptr;
+  if (a[2] != Py_None && !list_of(a[2], "keep_lens", 4, &entries_n)) return nullptr;
   if (!pointer(a[1], p) || !pointer(a[2], p + 1) || !stream_of(a[3], &stream)) return nullptr;
   return finish([&] {
     return ((decltype(&sp_pages_release))entries[kRelease].fn)(desc.table(), (const int32_t *)p[0], (const int32_t *)p[1], entries_n, stream);
@@ -418,11 +467,18 @@ PyObject *pages_release(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
   Desc desc;
   void *p[6], *stream;
-  int32_t table[2], sizes[4];
+  int32_t table[2], sizes[4] = {-1, -1, -1, -1};
+  int64_t step[2];
   size_t ws_bytes;
   if (!count("pages_compact", n, 8, kCompact) || !dims(a[1], table, 2, true) || !bytes_of(a[6], &ws_bytes) || !desc.take_table(a[0])) return nullptr;
+  if (!sized(a[1], "new_block_table", 4) || !steps_of(a[1], step, 2)) return nullptr;
+  if ((table[1] > 1 && step[1] != 1) || (table[0] > 1 && step[0] != table[1])) {
+    PyErr_SetString(PyExc_ValueError, "new_block_table: not contiguous");
+    return nullptr;
+  }
+  static const char *const names[] = {"new_ref_counts", "move_src", "move_dst", "moved"};
   for (int i = 0; i < 4; ++i)
-    if (!dims(a[2 + i], sizes + i, 1, true)) return nullptr;
+    if (!list_of(a[2 + i], names[i], 4, sizes + i)) return nullptr;
   const sp_page_table *t = desc.table();
   if (table[0] != t->num_rows || table[1] != t->max_pages_per_seq || sizes[0] != t->num_pages || sizes[1] < t->num_pages / 2 ||
       sizes[2] < t->num_pages / 2 || sizes[3] < 2) {
@@ -441,13 +497,10 @@ PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // (caches, src, dst, rows, count, stream): caches is a sequence
 PyObject *pages_copy(PyObject *, PyObject *const *a, Py_ssize_t n) {
   void *p[4], *stream;
-  int32_t pairs, more;
-  if (!count("pages_copy", n, 6, kCopy) || !dims(a[1], &pairs, 1, true)) return nullptr;
-  for (int i = 2; i < 4; ++i) {
-    if (i == 3 && a[3] == Py_None) continue;
-    if (!dims(a[i], &more, 1, true)) return nullptr;
-    if (more != pairs) return PyErr_Format(PyExc_ValueError, "%d sources, and an array of %d entries", (int)pairs, (int)more);
-  }
+  int32_t pairs = -1;
+  if (!count("pages_copy", n, 6, kCopy) || !list_of(a[1], "src", 4, &pairs) || !list_of(a[2], "dst", 4, &pairs) ||
+      (a[3] != Py_None && !list_of(a[3], "rows", 4, &pairs)) || !counters(a[4], "count", 1))
+    return nullptr;
   PyObject *fast = PySequence_Fast(a[0], "caches is not a sequence");
   if (!fast) return nullptr;
   const Py_ssize_t m = PySequence_Fast_GET_SIZE(fast);

@@ -266,3 +266,64 @@ def test_marshalling_refuses(seen):
 def test_no_exception_leaves_the_table_check():
     assert sp.lib().sp_debug_validate_pages(ctypes.byref(table(num_rows=2**31 - 1, max_pages_per_seq=2**31 - 1))) == UNSUPPORTED
     assert sp.lib().sp_debug_validate_pages(None) == NULL and sp.lib().sp_debug_validate_pages(ctypes.byref(table(num_pages=0))) == SHAPE
+
+
+def test_marshalling_refuses_other_types_and_shapes(seen):
+    """Lists of 64-bit numbers (torch's own whole numbers), strided lists, and lists shorter than what is read."""
+    c, t = Holder(cache()), Holder(table())
+    q, kv, out, bt, cu, ctx = T(1, 6, 8, 128, size=2), T(9, 6, 2, 128, size=2), T(2, 6, 8, 128, size=2), T(5, 2, 4), T(3, 3), T(4, 2)
+    good = dict(q=q, k=kv, v=kv, q_out=out, cu_seqlens_new=cu, ctx_lens=ctx, block_table=bt, q_weight=T(13, 128, size=2), k_weight=T(13, 128, size=2), cos_sin=T(14, 50, 64),
+                positions=T(15, 6))
+    sp.sp_norm_rope_append(c, **good, stream=0)
+    sp.sp_norm_rope_append(c, **{**good, "positions": T(15, 9), "cos_sin": T(14, 1, 64, strides=(99, 1))}, stream=0)
+    assert len(seen) == 2
+    bad = dict(
+        cu_seqlens_new=[T(3, 3, size=8)], ctx_lens=[T(4, 2, size=8)],
+        block_table=[T(5, 2, 4, size=8)],
+        q_weight=[T(13, 127, size=2), T(13, 129, size=2), T(13, 128), T(13, 128, size=2, strides=(2,)), T(13, 1, 128, size=2)],
+        k_weight=[T(13, 64, size=2), T(13, 128, size=8), T(13, 128, size=2, strides=(0,))],
+        cos_sin=[T(14, 50, 64, size=2), T(14, 50, 64, size=8), T(14, 50, 64, strides=(128, 1)), T(14, 50, 64, strides=(1, 50)), T(14, 50, 64, strides=(64, 2))],
+        positions=[T(15, 5), T(15, 6, size=8), T(15, 6, strides=(2,)), T(15, 6, 1)])
+    for name, values in bad.items():
+        for x in values:
+            with pytest.raises(ValueError):
+                sp.sp_norm_rope_append(c, **{**good, name: x}, stream=0)
+    with pytest.raises(ValueError):
+        sp.sp_norm_rope_append(c, None, None, None, None, cu, ctx, bt, stream=0)  # nothing to do it for
+    for i, x in enumerate((T(3, 3, size=8), T(4, 2, size=8), T(5, 2, 4, size=8))):
+        args = [cu, ctx, bt]
+        args[i] = x
+        with pytest.raises(ValueError):
+            sp.sp_attn_cross(c, q, out, *args, 3, 40, 0.5, stream=0)
+    ws, lists, one = T(0x9000, 64, size=1), [T(1, 3), T(2, 3)], T(3, 1)
+    for wrong in (T(1, 3, size=8), T(1, 3, size=2), T(1, 3, strides=(2,)), T(1, 3, strides=(0,)), T(1, 2), T(1, 4)):
+        for i in range(2):
+            args = list(lists)
+            args[i] = wrong
+            for call in (lambda: sp.sp_pages_reserve(t, *args, one, ws, stream=0), lambda: sp.sp_pages_release(t, *args, stream=0), lambda: sp.sp_pages_copy([c], *args, stream=0)):
+                with pytest.raises(ValueError):
+                    call()
+        for i in range(5):
+            args = [T(1, 3) for _ in range(5)]
+            args[i] = wrong
+            with pytest.raises(ValueError):
+                sp.sp_pages_fork(t, *args, one, ws, stream=0)
+        with pytest.raises(ValueError):
+            sp.sp_pages_copy([c], *lists, rows=wrong, stream=0)
+    for wrong in (T(3, 1, size=8), T(3, 0)):
+        for call in (lambda: sp.sp_pages_reserve(t, *lists, wrong, ws, stream=0), lambda: sp.sp_pages_fork(t, *[T(1, 3)] * 5, wrong, ws, stream=0),
+                     lambda: sp.sp_pages_copy([c], *lists, count=wrong, stream=0)):
+            with pytest.raises(ValueError):
+                call()
+    moves = [T(1, 4, 9), T(2, 100), T(3, 50), T(4, 50), T(5, 2)]
+    for i, values in enumerate(((T(1, 4, 9, size=8), T(1, 4, 9, strides=(18, 1)), T(1, 4, 9, strides=(1, 4))), (T(2, 100, size=8),), (T(3, 50, strides=(2,)),), (T(4, 50, size=2),),
+                                (T(5, 2, size=8),))):
+        for wrong in values:
+            args = list(moves)
+            args[i] = wrong
+            with pytest.raises(ValueError):
+                sp.sp_pages_compact(t, *args, ws, stream=0)
+    assert len(seen) == 2
+    sp.sp_pages_reserve(t, *lists, T(3, size=4), ws, stream=0)  # one counter without dimensions
+    sp.sp_pages_compact(t, *moves, ws, stream=0)
+    assert len(seen) == 4
