@@ -296,7 +296,9 @@ int sp_norm_rope_append(const sp_cache_desc *cache, const void *q, const void *k
  * Free pages are always taken in ascending order, for the entries of a call's list in their order: results do not
  * depend on timing.
  * Out-of-range rows and page ids are skipped; lengths count as at most max_pages_per_seq * 16.  Calls on one table are
- * ordered by the caller (one stream, or events between them).  With n = 0 nothing is done, and nothing written.
+ * ordered by the caller (one stream, or events between them).  With n = 0 nothing is done, and nothing written.  Lists of
+ * sp_pages_reserve, sp_pages_fork and sp_pages_release, and tables that are compacted, have up to 16000000 entries, or rows.
+ * Workspaces begin on a 16-byte boundary.
  *
  * Tokens are appended to pages that no other row holds.  What sp_pages_reserve adds is a row's own until a fork shares it, and a
  * fork shares the row's full pages of written tokens and nothing behind them.  It takes the written tokens from written_lens.  Without

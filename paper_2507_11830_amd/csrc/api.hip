@@ -236,6 +236,12 @@ static int check_table(const sp_page_table *t) {
   return SP_OK;
 }
 
+// A workgroup of 256 threads per entry, or per row: a launch has fewer than 2^32 threads.  Asked before the first of a call's launches.
+constexpr int kMostEntries = 16000000;
+static int check_entries(const char *name, int n) {
+  return n <= kMostEntries ? SP_OK : fail(SP_ERR_UNSUPPORTED, "%s: %d entries (at most %d)", name, n, kMostEntries);
+}
+
 static int check_pages_workspace(const char *name, const sp_page_table *t, int n, const void *workspace, size_t bytes) {
   const size_t need = pages_workspace_bytes(t->num_pages, n);
   if (!workspace || bytes < need) return fail(SP_ERR_WORKSPACE, "%s workspace: need %zu bytes, got %zu", name, need, workspace ? bytes : (size_t)0);
@@ -249,6 +255,7 @@ int sp_pages_reserve(const sp_page_table *table, const int32_t *rows, const int3
   if (n < 0) return fail(SP_ERR_BAD_SHAPE, "negative count in sp_pages_reserve");
   if (n == 0) return SP_OK;
   if (!rows || !new_lens || !shortfall) return fail(SP_ERR_NULL, "sp_pages_reserve: NULL argument");
+  if (int rc = check_entries("sp_pages_reserve", n)) return rc;
   if (int rc = check_pages_workspace("sp_pages_reserve", table, n, workspace, workspace_bytes)) return rc;
   return launch_pages_reserve(*table, rows, new_lens, n, shortfall, workspace, (hipStream_t)stream);
 }
@@ -259,6 +266,7 @@ int sp_pages_fork(const sp_page_table *table, const int32_t *parents, const int3
   if (n < 0) return fail(SP_ERR_BAD_SHAPE, "negative count in sp_pages_fork");
   if (n == 0) return SP_OK;
   if (!parents || !children || !copy_src || !copy_dst || !copy_rows || !shortfall) return fail(SP_ERR_NULL, "sp_pages_fork: NULL argument");
+  if (int rc = check_entries("sp_pages_fork", n)) return rc;
   if (int rc = check_pages_workspace("sp_pages_fork", table, n, workspace, workspace_bytes)) return rc;
   return launch_pages_fork(*table, parents, children, n, copy_src, copy_dst, copy_rows, shortfall, workspace, (hipStream_t)stream);
 }
@@ -268,6 +276,7 @@ int sp_pages_release(const sp_page_table *table, const int32_t *rows, const int3
   if (n < 0) return fail(SP_ERR_BAD_SHAPE, "negative count in sp_pages_release");
   if (n == 0) return SP_OK;
   if (!rows) return fail(SP_ERR_NULL, "sp_pages_release: NULL argument");
+  if (int rc = check_entries("sp_pages_release", n)) return rc;
   return launch_pages_release(*table, rows, keep_lens, n, (hipStream_t)stream);
 }
 
@@ -277,6 +286,7 @@ int sp_pages_compact(const sp_page_table *table, int32_t *new_block_table, int32
   if ((table->num_rows > 0 && table->max_pages_per_seq > 0 && !new_block_table) || !new_ref_counts || !moved ||
       (table->num_pages > 1 && (!move_src || !move_dst)))
     return fail(SP_ERR_NULL, "sp_pages_compact: NULL argument");
+  if (int rc = check_entries("sp_pages_compact, rows", table->num_rows)) return rc;
   if (int rc = check_pages_workspace("sp_pages_compact", table, 0, workspace, workspace_bytes)) return rc;
   return launch_pages_compact(*table, new_block_table, new_ref_counts, move_src, move_dst, moved, workspace, (hipStream_t)stream);
 }

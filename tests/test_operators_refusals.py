@@ -327,3 +327,13 @@ def test_marshalling_refuses_other_types_and_shapes(seen):
     sp.sp_pages_reserve(t, *lists, T(3, size=4), ws, stream=0)  # one counter without dimensions
     sp.sp_pages_compact(t, *moves, ws, stream=0)
     assert len(seen) == 4
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_more_entries_than_a_launch_holds(name):
+    """Refused before the first launch of the call, not by the one that cannot be made."""
+    if name == "compact":
+        assert pages_call(name, table(num_rows=16000001)) == UNSUPPORTED
+    else:
+        assert pages_call(name, n=16000001) == UNSUPPORTED and pages_call(name, n=2**31 - 1) == UNSUPPORTED
+    assert b"16000000" in sp.lib().sp_last_error()
