@@ -47,6 +47,16 @@ static int check_scale(float scale) {
   return SP_OK;
 }
 
+// What the checks of device arrays do on the host.  No exception crosses the ABI: host memory may not hold arrays of the sizes asked for.
+template <typename Check>
+static int checked(const char *name, Check check) {
+  try {
+    return check();
+  } catch (const std::exception &) {
+    return fail(SP_ERR_UNSUPPORTED, "%s: no host memory for arrays of these sizes", name);
+  }
+}
+
 }  // namespace sp
 
 using namespace sp;
@@ -332,11 +342,7 @@ static int validate_pages(const sp_page_table *table) {
 
 int sp_debug_validate_pages(const sp_page_table *table) {
   if (int rc = check_table(table)) return rc;
-  try {
-    return validate_pages(table);
-  } catch (const std::exception &) {  // no exception crosses the ABI
-    return fail(SP_ERR_UNSUPPORTED, "sp_debug_validate_pages: no host memory for %d rows of %d pages", table->num_rows, table->max_pages_per_seq);
-  }
+  return checked("sp_debug_validate_pages", [&] { return validate_pages(table); });
 }
 
 static int ulysses_common(bool pack, const void *src, void *dst, int32_t tokens, int32_t num_heads,
@@ -379,9 +385,8 @@ size_t sp_attn_decode_workspace_size(int32_t batch, int32_t max_seq_len, int32_t
   return decode_workspace_bytes(batch, max_seq_len, num_q_heads, head_dim);
 }
 
-int sp_debug_validate_metadata(const sp_cache_desc *cache, const int32_t *seq_lens,
-                               const int32_t *block_table, int32_t batch,
-                               int32_t max_pages_per_seq) {
+static int validate_metadata(const sp_cache_desc *cache, const int32_t *seq_lens,
+                             const int32_t *block_table, int32_t batch, int32_t max_pages_per_seq) {
   if (int rc = check_cache(cache)) return rc;
   if (batch < 0 || max_pages_per_seq < 0) return fail(SP_ERR_BAD_SHAPE, "negative count");
   if (batch == 0) return SP_OK;
@@ -406,8 +411,8 @@ int sp_debug_validate_metadata(const sp_cache_desc *cache, const int32_t *seq_le
   return SP_OK;
 }
 
-int sp_debug_validate_hints(const int32_t *cu_seqlens, const int32_t *lens, int32_t batch, int32_t total_tokens,
-                            int32_t max_q_len, int32_t max_len) {
+static int validate_hints(const int32_t *cu_seqlens, const int32_t *lens, int32_t batch, int32_t total_tokens,
+                          int32_t max_q_len, int32_t max_len) {
   if (batch < 0) return fail(SP_ERR_BAD_SHAPE, "negative batch");
   if (batch == 0) return SP_OK;
   if (!lens) return fail(SP_ERR_NULL, "NULL length array");
@@ -433,6 +438,16 @@ int sp_debug_validate_hints(const int32_t *cu_seqlens, const int32_t *lens, int3
       return fail(SP_ERR_BAD_SHAPE, "sequence %d reaches %ld keys > the length hint %d", s, reach, max_len);
   }
   return SP_OK;
+}
+
+int sp_debug_validate_metadata(const sp_cache_desc *cache, const int32_t *seq_lens, const int32_t *block_table, int32_t batch,
+                               int32_t max_pages_per_seq) {
+  return checked("sp_debug_validate_metadata", [&] { return validate_metadata(cache, seq_lens, block_table, batch, max_pages_per_seq); });
+}
+
+int sp_debug_validate_hints(const int32_t *cu_seqlens, const int32_t *lens, int32_t batch, int32_t total_tokens, int32_t max_q_len,
+                            int32_t max_len) {
+  return checked("sp_debug_validate_hints", [&] { return validate_hints(cu_seqlens, lens, batch, total_tokens, max_q_len, max_len); });
 }
 
 int sp_debug_set_tuning(const char *key, int32_t value) {

@@ -337,3 +337,8 @@ def test_more_entries_than_a_launch_holds(name):
     else:
         assert pages_call(name, n=16000001) == UNSUPPORTED and pages_call(name, n=2**31 - 1) == UNSUPPORTED
     assert b"16000000" in sp.lib().sp_last_error()
+
+
+def test_no_exception_leaves_the_metadata_check():
+    assert sp.lib().sp_debug_validate_metadata(ctypes.byref(cache()), P, P, 65536, 2**31 - 1) == UNSUPPORTED
+    assert b"memory" in sp.lib().sp_last_error()
