@@ -414,3 +414,105 @@ def test_pages_beyond_four_gigabytes():
             got.append(torch.full_like(x, float("nan")))
             sp.sp_attn_cross(cache, x, got[-1], ends, lens, table, longest, most, 0.09)
         assert torch.equal(got[0].view(torch.int16), got[1].view(torch.int16)) and torch.isfinite(got[0]).all()
+
+
+EVERY_KEY = [
+    ((8, 1, 128), [1], [30000]),  # shares and their merge
+    ((32, 8, 128), [2, 1], [9000, 5]),
+    ((12, 3, 64), [1] * 600, "uneven"),  # more sequences than shares are dealt for
+    ((8, 1, 128), [1] * 64, "uneven"),  # splits of the longest range
+    ((16, 2, 64), [4] * 32, "uneven"),
+    ((8, 1, 128), [40, 70], [9000, 6000]),  # pieces
+    ((16, 2, 64), [100], [12000]),
+    ((8, 1, 128), [8], [60000]),  # column tiles
+    ((12, 3, 64), [9, 100, 17], [512, 130, 333]),
+    ((8, 1, 128), [5000, 10, 40], [128, 97, 0]),  # keys that stay in LDS
+    ((32, 8, 128), [1500, 1400, 1490], [320, 257, 31]),
+    ((8, 1, 128), [2000, 2500], [640, 512]),  # two workgroups a CU
+    ((12, 3, 64), [600, 17, 300], [2500, 65, 700]),  # halves
+    ((8, 1, 128), [1000] * 6, [1700, 0, 1900, 400, 1500, 64]),  # whole tiles
+]
+
+
+@pytest.mark.parametrize("edges", (False, True), ids=("blocks", "first-and-last-of-32"))
+@pytest.mark.parametrize("heads,nq,nk", EVERY_KEY, ids=lambda x: "x".join(map(str, x[:3])) if isinstance(x, (list, tuple)) else str(x))
+def test_every_block_of_keys_counts_once(heads, nq, nk, edges):
+    """All scores are 0, so all weights are 1, which bf16 holds.  A block of 32 keys (or the first and the last key of one) has values of 1 in one channel,
+    the next block in the next, and so on: a block that is lost, or taken twice, moves its channel by 1 / (blocks of that channel), asserted to be
+    several times the only rounding there is, half a bf16 step (2^-8)."""
+    nk = [int(x) for x in np.random.default_rng(3).integers(100, 2000, len(nq))] if nk == "uneven" else nk
+    if len(nq) > 30:
+        nk[3] = nk[17] = 0
+    c = Case(heads, nq, nk, seed=21)
+    k, v = c.cache.k_pages, c.cache.v_pages
+    for p in (k, v):
+        p.copy_(torch.where(torch.isnan(p), p, torch.zeros((), dtype=p.dtype, device="cuda")))
+    wants = []
+    for s, n in enumerate(nk):
+        pos = torch.arange(n, device="cuda")
+        item = pos // 32
+        if edges:
+            chosen = (pos % 32 == 0) | (pos % 32 == 31) | (pos == n - 1)
+            pos, item = pos[chosen], torch.arange(int(chosen.sum()), device="cuda")
+        page = c.table[s].long()[pos // 16]
+        want = torch.zeros(c.hkv, c.d, dtype=torch.float64, device="cuda")
+        items = torch.zeros(c.d, device="cuda").index_add_(0, torch.unique(item) % c.d, torch.ones(len(torch.unique(item)), device="cuda"))
+        assert items.max() <= 2**5  # one of them is 2^-5 of the channel, eight times the rounding
+        for h in range(c.hkv):
+            channel = (item + 7 * h) % c.d
+            v[page, h, pos % 16, channel] = 1
+            want[h].index_add_(0, channel, torch.full((len(pos),), 1 / max(n, 1), dtype=torch.float64, device="cuda"))
+        wants.append(want.repeat_interleave(c.hq // c.hkv, dim=0))
+    for ws in (c.workspace(), None):
+        c.out.fill_(float("nan"))
+        c.call(ws)
+        for s in range(len(nk)):
+            got = c.out[int(c.cu[s]):int(c.cu[s + 1])].double()
+            assert ((got - wants[s]).abs() <= (2.0**-8 + 2.0**-20) * wants[s]).all(), s
+
+
+@pytest.mark.parametrize("spread", (4.0, 16.0))
+@pytest.mark.parametrize("heads,nq,nk", [
+    ((8, 1, 128), [300, 7, 0, 65], [64, 33, 30, 0]), ((8, 1, 128), [5000, 10, 40], [128, 97, 0]), ((32, 8, 128), [1500, 33, 600], [256, 129, 31]),
+    ((32, 8, 128), [1500, 1400, 1490], [320, 257, 31]), ((16, 2, 64), [4000, 1], [200, 255]), ((7, 1, 64), [50, 3], [33, 100]), ((32, 8, 128), [3, 1] * 20, [100, 7] * 20),
+], ids=lambda x: "x".join(map(str, x[:3])))
+def test_scores_far_beyond_the_first_block_s_in_lds(heads, nq, nk, spread):
+    """Keys that stay in LDS, rows whose maximum moves from block to block.  A score is a sum of d products in fp32, off by at most d * 2^-24 of
+    the sum of their magnitudes (A); its weight by that times the scale, the output by twice that of sum(w |v|).  Weights as hi + lo: 2^-16, or bf16 (2^-8)
+    beyond 256 keys; fp32 sums of up to 320 of them: 2^-15.  Half a bf16 step of the output: 2^-8."""
+    c = Case(heads, nq, nk, seed=22, spread=spread)
+    assert c.workspace() is None
+    c.call(None)
+    for s in range(len(nk)):
+        a, b = int(c.cu[s]), int(c.cu[s + 1])
+        if a == b or nk[s] == 0:
+            assert (c.out[a:b] == 0).all()
+            continue
+        want, size = c.definition(s)
+        pos = torch.arange(nk[s], device="cuda")
+        keys = c.cache.k_pages[c.table[s].long()[pos // 16], :, pos % 16].double().abs()  # [keys, KV heads, d]
+        rows = c.q[a:b].double().abs().view(b - a, c.hkv, -1, c.d)
+        most = max(float((rows[:, h].reshape(-1, c.d) @ keys[:, h].t().contiguous()).max()) for h in range(c.hkv))
+        off = 2 * c.d * 2.0**-24 * most * c.scale + 2.0**-15 + (2.0**-8 if nk[s] > 256 else 2.0**-16)
+        got = c.out[a:b].double()
+        assert torch.isfinite(got).all() and ((got - want).abs() <= 2.0**-8 * want.abs() + off * size).all(), s
+
+
+def test_more_keys_than_the_hint_in_lds():
+    """Sequences longer than the hint that sizes the LDS: any number of states between the hint and the length, none behind the table's row."""
+    for heads, nq, nk in (((8, 1, 128), [300, 7, 65], [64, 10, 33]), ((32, 8, 128), [1500, 33, 600], [256, 129, 31]), ((16, 2, 64), [4000, 1], [200, 255]), ((7, 1, 64), [50, 3], [33, 100])):
+        c = Case(heads, nq, nk, seed=23)
+        for p in (c.cache.k_pages, c.cache.v_pages):
+            p.nan_to_num_(0.25)
+        c.table.clamp_(min=0)
+        hint, width = c.max_kv, 16 * c.table.shape[1]
+        c.lens += 1000
+        c.call(None)
+        for s, n in enumerate(nq):
+            got, ok = c.out[int(c.cu[s]):int(c.cu[s + 1])].double(), None
+            for keys in range(min(hint, width), width + 1):
+                c.nk[s] = keys
+                want, size = c.definition(s)
+                fits = ((got - want).abs() <= 2.0**-8 * want.abs() + (2.0**-13 + 2.0**-8) * size).flatten(1).all(1)
+                ok = fits if ok is None else ok | fits
+            assert ok.all(), s

@@ -552,3 +552,16 @@ def test_parent_and_child_go_on_in_pages_of_their_own(pad, cut):
         page = b.t.block_table[row].long()[pos // 16]
         for pool in (cache.k_pages, cache.v_pages):
             assert torch.equal(pool[page, :, pos % 16], tokens[row])
+
+
+@pytest.mark.parametrize("heads,d", [(1, 64), (1, 128), (3, 64)])
+def test_more_rows_than_a_page_has(heads, d):
+    """Whole pages, and nothing of the page behind."""
+    caches, n = make_caches(2, 40, heads, d), 13
+    perm = np.random.default_rng(4).permutation(40)
+    src, dst, rows = perm[:n], perm[n:2 * n], [99, 16, 17, 2**31 - 1, 15, 0, -1] + [1] * 6
+    pools = [p for c in caches for p in (c.k_pages, c.v_pages)]
+    want = copied(pools, src, dst, [min(max(r, 0), 16) for r in rows])
+    sp.sp_pages_copy(caches, dev(src), dev(dst), rows=dev(rows), count=dev([n]))
+    for p, w in zip(pools, want):
+        assert torch.equal(p.view(torch.int16), w)
