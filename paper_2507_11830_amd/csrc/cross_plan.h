@@ -19,7 +19,7 @@ constexpr int kCus = 256;
 struct CrossShape {
   bool halves;  // 128 columns, whose keys two wave groups share; else whole tiles of 256 (head_dim 64: 128, three workgroups a CU)
   bool solo;    // head_dim 128: 128 columns, two workgroups a CU
-  bool ranked;  // workgroups take the longest items first; else in (tile, sequence) order
+  bool ranked;  // workgroups take their items by keys plus the tile's place in its chunk, most first (the causal calls' weight); else in (tile, sequence) order
   int pieces;   // of the key ranges (halves only)
 };
 
@@ -85,9 +85,9 @@ inline bool cross_resident_for_few(long streams, long max_kv_len, int head_dim) 
 
 // Chunks of a few column tiles of a wave (q_cap tokens each): every tile in a workgroup of the decode kernel of its own, which reads the
 // keys again but begins in a third of the time that a query tile takes.  Up to 512 keys each in one launch, where the workgroups are
-// one round (240 batches: 1.28 times as fast in the mean, the worst 0.93; 2 x 16 tokens on 278 keys at 32q/8kv 11.4 -> 7.9 us); longer ranges
+// one round (240 batches: 1.28 times as fast in the mean, the worst 0.93); longer ranges
 // in splits that are merged, for few workgroups and keys (about 170 batches: 1.12 times, six of them more than 5 % slower; 1 x 64 tokens on
-// 2616 at 32q/4kv 14.8 -> 12.0, but 15 x 33 on 516 at 12q/3kv, head_dim 64, 9.5 and 13.4).
+// 2000 at 32q/4kv 18.6 -> 16.1, 1 x 32 on 2616 16.2 -> 14.8, but 15 x 33 on 516 at 12q/3kv, head_dim 64, 9.5 and 13.4).
 struct CrossTiles {
   int tiles;  // 0: not taken
   int splits, chunk;
@@ -161,8 +161,8 @@ inline CrossShape cross_shape(long rows, int batch, long streams, int columns, l
   // Two workgroups of 128 columns on a CU, whose starts and stores are behind each other's multiplications: a tile takes 0.62 us per workgroup
   // there, one alone 0.8; starts 4 us a round.  Where every workgroup of 128 columns has a CU to itself the halves are faster (500 batches: by
   // 2 to 25 %, the more keys the more).  On more tiles than about 32 whole tiles, which load every key once per 256 columns,
-  // are as fast or faster.  873 batches on 257 to 6000 keys: 2 % over the best of all forms, 10 % without this one; 12 x 1212 queries on 272
-  // keys at 32q/4kv 151 -> 107 us, 7 x 313 on 529 41.7 -> 31.5; but 6 x 714 on 2014 at 8q/1kv 45.6 and 51.9.
+  // are as fast or faster.  873 batches on 257 to 6000 keys: 2 % over the best of all forms, 10 % without this one; 12 x 1212 queries on 340
+  // keys at 32q/4kv 163 -> 121 us, 7 x 313 on 529 46 -> 36; but 6 x 714 on 2014 at 8q/1kv 45.6 and 51.9.
   const long full = (long)n / (2 * kCus), left = ceil_div((long)n % (2 * kCus), kCus);
   double solo;
   if (uneven) {
