@@ -95,6 +95,11 @@ bool steps_of(PyObject *t, int64_t *out, Py_ssize_t n) {
   return !PyErr_Occurred();
 }
 
+// A matrix of these sizes and strides whose rows follow each other; an empty one does whatever its strides say.
+bool contiguous(const int32_t *size, const int64_t *step) {
+  return size[0] == 0 || size[1] == 0 || ((size[1] == 1 || step[1] == 1) && (size[0] == 1 || step[0] == size[1]));
+}
+
 // Elements of the width that is read: whole numbers of 4 bytes (torch's own have 8), angles of 4, weights of 2.
 bool sized(PyObject *t, const char *name, long bytes) {
   PyObject *e = PyObject_CallMethodNoArgs(t, s_element_size);
@@ -388,7 +393,7 @@ PyObject *norm_rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (a[11] != Py_None) {
     int64_t step[2];
     if (!dims(a[11], angles, 2, true) || !sized(a[11], "cos_sin", 4) || !steps_of(a[11], step, 2)) return nullptr;
-    if ((angles[1] > 1 && step[1] != 1) || (angles[0] > 1 && step[0] != angles[1])) {
+    if (!contiguous(angles, step)) {
       PyErr_SetString(PyExc_ValueError, "cos_sin: not contiguous");
       return nullptr;
     }
@@ -472,7 +477,7 @@ PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
   size_t ws_bytes;
   if (!count("pages_compact", n, 8, kCompact) || !dims(a[1], table, 2, true) || !bytes_of(a[6], &ws_bytes) || !desc.take_table(a[0])) return nullptr;
   if (!sized(a[1], "new_block_table", 4) || !steps_of(a[1], step, 2)) return nullptr;
-  if ((table[1] > 1 && step[1] != 1) || (table[0] > 1 && step[0] != table[1])) {
+  if (!contiguous(table, step)) {
     PyErr_SetString(PyExc_ValueError, "new_block_table: not contiguous");
     return nullptr;
   }

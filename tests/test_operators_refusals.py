@@ -342,3 +342,13 @@ def test_more_entries_than_a_launch_holds(name):
 def test_no_exception_leaves_the_metadata_check():
     assert sp.lib().sp_debug_validate_metadata(ctypes.byref(cache()), P, P, 65536, 2**31 - 1) == UNSUPPORTED
     assert b"memory" in sp.lib().sp_last_error()
+
+
+def test_marshalling_takes_empty_matrices(seen):
+    """Whatever their strides say (torch gives a table of 5 rows and no columns those of one column)."""
+    t = Holder(table(max_pages_per_seq=0))
+    t.desc.num_rows = 5
+    sp.sp_pages_compact(t, T(1, 5, 0, strides=(1, 1)), T(2, 100), T(3, 50), T(4, 50), T(5, 2), T(0x9000, 64, size=1), stream=0)
+    q, out = T(1, 6, 8, 128, size=2), T(2, 6, 8, 128, size=2)
+    sp.sp_norm_rope_append(Holder(cache()), q, None, None, out, T(3, 3), T(4, 2), None, cos_sin=T(14, 50, 0, strides=(1, 1)), stream=0)
+    assert [name for name, _ in seen] == ["sp_pages_compact", "sp_norm_rope_append"] and seen[1][1][11].rotary_dim == 0
