@@ -8,8 +8,9 @@
 // Bound: HBM (queries in, outputs out) up to about 100 keys.  Beyond, neither a pipe nor a memory, but a wave's chain of scores, weights and
 // products, which the one other wave on its SIMD covers in part: on 8 x 1749 queries on 229 keys at 16q/2kv (56 us, floor 24) the matrix pipe
 // is busy in 41 % of the CU cycles and the LDS in 21, on 12 x 957 on 259 at 32q/8kv (87 us, floor 41) in 35 and 19; rows of up to 256 keys
-// multiply their weights as hi + lo, half as many operations again.  Measured (query tiles -> here): 13 x 3331 queries on 18 keys at 32q/8kv, head_dim 128, 318 -> 173 us (0.71 GB,
-// 4.1 TB/s); 7 x 1901 on 26 89 -> 41; 1 x 57 on 10 at 8q/1kv 10.9 -> 5.8; 14 x 4489 on 90 at 16q/2kv, head_dim 64, 96 -> 71.
+// multiply their weights as hi + lo, half as many operations again.  Measured (query tiles -> here): 13 x 3331 queries on 18 keys at
+// 32q/8kv, head_dim 128, 315 -> 146 us (0.71 GB, 4.9 TB/s); 7 x 1901 on 26 88 -> 40; 1 x 57 on 10 at 8q/1kv 10.9 -> 5.8; 14 x 4489 on 90 at
+// 16q/2kv, head_dim 64, 96 -> 64.
 #include "decode_block.h"
 #include "prefill_tile.h"
 #include "cross_plan.h"
